@@ -333,6 +333,48 @@ int bn_bwd_batchstats(int n, int c, int h, int w, int layout,
                       void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Group normalization (Wu and He 2018): like batch normalization, with the statistics of `groups` runs of C/groups
+ * neighbouring channels of ONE image, so that a result does not depend on how many images a GPU has, and validation
+ * needs no saved statistics.  Per image n and group g, over its m = H*W*C/groups values:
+ *   mean = (1/m) sum x,  var = (1/m) sum (x-mean)^2,  invstd = 1/sqrt(var + eps),  xhat = (x-mean)*invstd
+ *   u = gamma[c]*xhat + beta[c]  [+ residual],   y = act(u)
+ * RN50_ACT_RELU: max(0, u).  RN50_ACT_SILU: u / (1 + exp(-u)).
+ * x, y, residual, dy, dy2, dx, dresidual: N x H x W x C (the _bf16 calls: bfloat16 bits, widened exactly on load, all
+ * arithmetic and every sum fp32, one rounding to nearest even per stored value).  gamma, beta, dgamma, dbeta: C floats;
+ * save_mean, save_invstd: N x groups floats (both NULL where no backward pass follows).  C % 4 == 0, C % groups == 0,
+ * H*W*C and N*C below 2^31 (else RN50_EUNSUPPORTED; groups that do not divide C: RN50_EINVAL).  Outputs do not overlap
+ * inputs.  A NaN or an infinity in a group makes that group's outputs NaN and no other's.  Results are bit-identical
+ * from call to call.
+ * ------------------------------------------------------------------------------------------ */
+#define RN50_ACT_NONE 0
+#define RN50_ACT_RELU 1
+#define RN50_ACT_SILU 2
+
+/* Scratch of the four calls for this shape (0 for invalid arguments: the call itself reports the error). */
+size_t rn50_gn_workspace_bytes(int n, int c, int h, int w, int groups);
+
+int gn_fwd(int n, int c, int h, int w, int layout, int groups, const float *x, const float *gamma, const float *beta, float eps,
+           const float *residual_or_null, int act, float *y, float *save_mean_or_null, float *save_invstd_or_null,
+           void *ws, size_t ws_bytes, void *stream);
+int gn_fwd_bf16(int n, int c, int h, int w, int layout, int groups, const uint16_t *x, const float *gamma, const float *beta, float eps,
+                const uint16_t *residual_or_null, int act, uint16_t *y, float *save_mean_or_null, float *save_invstd_or_null,
+                void *ws, size_t ws_bytes, void *stream);
+
+/* Backward of the above.  The incoming gradient is dy (+ dy2 when not NULL, the second consumer's).  u is formed again from
+ * x, the saved statistics and the residual with the forward pass's roundings, so the ReLU mask is [u > 0] of the forward
+ * pass (derivative at exactly 0 is 0) and y is not read; residual_or_null has to be the forward's (it is not needed with
+ * RN50_ACT_NONE, and may be NULL then).
+ *   dz = (dy + dy2) * act'(u),  dresidual = dz  (written when dresidual_or_null != NULL)
+ *   dbeta = sum over n,h,w of dz,  dgamma = sum over n,h,w of dz*xhat
+ *   dx = invstd * (gamma*dz - (1/m) sum gamma*dz - xhat * (1/m) sum gamma*dz*xhat)   (sums over the image's group) */
+int gn_bwd(int n, int c, int h, int w, int layout, int groups, const float *x, const float *dy, const float *dy2_or_null,
+           const float *residual_or_null, const float *gamma, const float *beta, const float *save_mean, const float *save_invstd,
+           int act, float *dx, float *dresidual_or_null, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream);
+int gn_bwd_bf16(int n, int c, int h, int w, int layout, int groups, const uint16_t *x, const uint16_t *dy, const uint16_t *dy2_or_null,
+                const uint16_t *residual_or_null, const float *gamma, const float *beta, const float *save_mean, const float *save_invstd,
+                int act, uint16_t *dx, uint16_t *dresidual_or_null, float *dgamma, float *dbeta, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------
  * The remaining layers of ResNet-50 (He et al. 2016), NHWC.
  * ------------------------------------------------------------------------------------------ */
 /* 3x3 / stride 2 / pad 1 max pooling (padding never wins).  y is N x P x Q x C with P = (H-1)/2+1.
@@ -368,6 +410,50 @@ int fc_bwd(int n, int j, int k, const float *f, const float *w, const float *dy,
  * dlogits = (softmax - onehot)/N.  labels: N int32 in [0,K) on the device (a label outside that range is not an error
  * code, since the labels are device memory: it makes the loss NaN and contributes no one-hot term).  N <= 1024. */
 int softmax_ce(int n, int k, const float *logits, const int32_t *labels, float *loss, float *dlogits, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Learning from a teacher (Hinton et al. 2015) of which only the largest logits of each row are kept.
+ * logits: N rows of K classes, row n starting at logits + n*ld elements (ld >= K: a row may be padded; what lies behind
+ * its K classes is neither read nor written).  The _bf16 calls take logits (and write their gradient) as bfloat16 bits;
+ * everything else is fp32.  Rows of any length, fewer than 2^22 of them;
+ * t in [1, RN50_TOPK_MAX].
+ * ------------------------------------------------------------------------------------------ */
+#define RN50_TOPK_MAX 256
+
+/* val[n][0..t), idx[n][0..t): the t largest logits of each row (t <= K) and their classes, in falling order; equal logits
+ * by rising class (-0 and 0 are equal).  A NaN counts as larger than any number, as all of them equal.  Values are the
+ * logits themselves, widened exactly. */
+size_t rn50_topk_workspace_bytes(int n, int k, int t);
+int logits_topk(int n, int k, int t, const float *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes, void *stream);
+int logits_topk_bf16(int n, int k, int t, const uint16_t *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes,
+                     void *stream);
+
+/* Cross-entropy with the label and with the teacher's kept logits at temperature tau.  Row n, with q = softmax(z),
+ * r = softmax(z/tau) over all K classes and p = softmax(val/tau) over the row's kept entries (class idx[t] each):
+ *   hard = -log q[label]              (0 for label -1: a row without a label)
+ *   soft = tau^2 * sum_t p_t * (log p_t - log r[idx_t])     (0 for a row that keeps nothing)
+ *   loss[0] = (1-alpha)*loss[1] + alpha*loss[2],  loss[1] = scale * sum_n hard,  loss[2] = scale * sum_n soft
+ *   dlogits[n][k] = scale * ((1-alpha)*(q_k - [k == label]) [rows with a label]
+ *                            + alpha*tau*(r_k - sum of p_t with idx_t == k) [rows that keep something])
+ * scale: 1/N for softmax_ce's mean, 1/(rows that count) where some are padding.  alpha in [0, 1]: with alpha == 1 labels may
+ * be NULL (and are not looked at: loss[1] is 0), with alpha == 0 the teacher is not looked at (t may be 0, teacher_idx and
+ * teacher_val NULL; loss[2] is 0).  tau in [1/1024, 1024].
+ * labels: N int32; teacher_idx, teacher_val: N x t, rows one behind the other (logits_topk's output).  An index of -1 or a
+ * kept logit of -infinity keeps nothing; a class that occurs twice in a row counts twice.  Any other label or index outside
+ * [0, K) is no error code (they are device memory): it makes the loss NaN and contributes no term to the gradient.  A class
+ * masked by -infinity or the type's lowest value has q = r = 0 and no gradient of its own; where the label or a kept class is
+ * masked by -infinity, the loss is infinite and the gradient finite.  A row of nothing but -infinity, or with a NaN or
+ * +infinity, has NaN for its gradient and makes the loss NaN.  A row that has no label and keeps nothing counts for nothing,
+ * whatever its logits: its gradient is 0.
+ * loss: 3 floats.  dlogits: row n at dlogits + n*ld_dlogits (ld_dlogits >= K), not in place; NULL: the loss alone.
+ * Results are bit-identical from call to call. */
+size_t rn50_distill_workspace_bytes(int n, int k, int t);
+int distill_ce(int n, int k, int t, const float *logits, size_t ld, const int32_t *labels_or_null, const int32_t *teacher_idx,
+               const float *teacher_val, float alpha, float tau, float scale, float *loss, float *dlogits_or_null, size_t ld_dlogits,
+               void *ws, size_t ws_bytes, void *stream);
+int distill_ce_bf16(int n, int k, int t, const uint16_t *logits, size_t ld, const int32_t *labels_or_null, const int32_t *teacher_idx,
+                    const float *teacher_val, float alpha, float tau, float scale, float *loss, uint16_t *dlogits_or_null,
+                    size_t ld_dlogits, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------
  * Half-precision communication buffer (Section 3, "Software": compute in single precision,

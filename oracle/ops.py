@@ -222,3 +222,83 @@ def lr_base(n_workers, b_local):
 
 def lr_slow_start(epoch, n_workers=1024, b_local=32):
     return lib().orc_lr_slow_start(C.c_double(epoch), int(n_workers), int(b_local))
+
+
+# ---- group normalization, the largest logits, distillation: from their definitions, in 64 bits -----------------------------
+def _groups(v, g):
+    n, c, h, w = v.shape
+    return v.reshape(n, g, c // g, h, w)
+
+
+def _per_channel(stat, c):
+    """N x G as N x C x 1 x 1."""
+    return np.repeat(_d(stat), c // stat.shape[1], axis=1)[:, :, None, None]
+
+
+def _sigmoid(u):
+    return 0.5 * (1.0 + np.tanh(0.5 * u))
+
+
+def gn_fwd(x, groups, gamma, beta, eps, residual=None, act="none"):
+    """(y, mean, invstd), statistics N x G; act: "none", "relu" or "silu"."""
+    x = _d(x)
+    c = x.shape[1]
+    v = _groups(x, groups)
+    mean = v.mean(axis=(2, 3, 4))
+    invstd = 1.0 / np.sqrt(((v - mean[:, :, None, None, None]) ** 2).mean(axis=(2, 3, 4)) + eps)
+    u = (x - _per_channel(mean, c)) * _per_channel(invstd, c) * _d(gamma)[None, :, None, None] + _d(beta)[None, :, None, None]
+    if residual is not None:
+        u = u + _d(residual)
+    return {"none": lambda: u, "relu": lambda: np.maximum(u, 0.0), "silu": lambda: u * _sigmoid(u)}[act](), mean, invstd
+
+
+def gn_bwd(x, dy, groups, gamma, beta, mean, invstd, residual=None, act="none"):
+    """(dx, dz, dgamma, dbeta); dz is the gradient of the residual."""
+    x, c = _d(x), x.shape[1]
+    ch = lambda v: _d(v)[None, :, None, None]
+    xhat = (x - _per_channel(mean, c)) * _per_channel(invstd, c)
+    u = xhat * ch(gamma) + ch(beta)
+    if residual is not None:
+        u = u + _d(residual)
+    s = _sigmoid(u)
+    dz = _d(dy) * {"none": lambda: 1.0, "relu": lambda: (u > 0).astype(np.float64), "silu": lambda: s + u * s * (1 - s)}[act]()
+    a = dz * ch(gamma)
+    over = lambda v: np.repeat(_groups(v, groups).mean(axis=(2, 3, 4)), c // groups, axis=1)[:, :, None, None]
+    dx = (a - over(a) - xhat * over(a * xhat)) * _per_channel(invstd, c)
+    return dx, dz, (dz * xhat).sum(axis=(0, 2, 3)), dz.sum(axis=(0, 2, 3))
+
+
+def topk(logits, t):
+    """(values, classes) of the t largest of each row: falling, equal ones by rising class, NaN above every number."""
+    z = np.asarray(logits)
+    z = z.astype(np.float64) if z.dtype != np.float64 else z
+    k = np.arange(z.shape[1])
+    idx = np.stack([np.lexsort((k, -np.where(np.isnan(r), 0.0, r), ~np.isnan(r)))[:t] for r in z]).astype(np.int32)
+    return np.take_along_axis(z, idx, axis=1), idx
+
+
+def distill_ce(logits, labels, idx, val, alpha, tau, scale):
+    """(loss[3], dlogits).  labels or (idx, val) None: that term is left out.  Rows of finite logits or -inf."""
+    z = _d(logits)
+    grad, hard, soft = np.zeros_like(z), 0.0, 0.0
+
+    def log_softmax(v):
+        v = v - v.max()
+        return v - np.log(np.exp(v).sum())
+
+    for n, row in enumerate(z):
+        if labels is not None and labels[n] != -1:
+            log_q = log_softmax(row)
+            hard -= log_q[labels[n]]
+            grad[n] += (1 - alpha) * np.exp(log_q)
+            grad[n, labels[n]] -= 1 - alpha
+        if idx is not None:
+            keep = [(int(i), float(v)) for i, v in zip(idx[n], val[n]) if i != -1 and v != -np.inf]
+            if keep:
+                log_r, log_p = log_softmax(row / tau), log_softmax(np.array([v for _, v in keep]) / tau)
+                grad[n] += alpha * tau * np.exp(log_r)
+                for (i, _), lp in zip(keep, log_p):
+                    soft += tau * tau * np.exp(lp) * (lp - log_r[i])
+                    grad[n, i] -= alpha * tau * np.exp(lp)
+    hard, soft = hard * scale, soft * scale
+    return np.array([(1 - alpha) * hard + alpha * soft, hard, soft]), grad * scale

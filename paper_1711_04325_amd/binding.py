@@ -89,6 +89,17 @@ _SIGS = {
     "fc_fwd": (_i, [_i, _i, _i, _vp, _vp, _vp, _vp, _vp]),
     "fc_bwd": (_i, [_i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "softmax_ce": (_i, [_i, _i, _vp, _vp, _vp, _vp, _vp]),
+    "rn50_gn_workspace_bytes": (_sz, [_i] * 5),
+    "gn_fwd": (_i, [_i] * 6 + [_vp, _vp, _vp, _f, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gn_fwd_bf16": (_i, [_i] * 6 + [_vp, _vp, _vp, _f, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gn_bwd": (_i, [_i] * 6 + [_vp] * 8 + [_i] + [_vp] * 5 + [_sz, _vp]),
+    "gn_bwd_bf16": (_i, [_i] * 6 + [_vp] * 8 + [_i] + [_vp] * 5 + [_sz, _vp]),
+    "rn50_topk_workspace_bytes": (_sz, [_i] * 3),
+    "logits_topk": (_i, [_i] * 3 + [_vp, _sz, _vp, _vp, _vp, _sz, _vp]),
+    "logits_topk_bf16": (_i, [_i] * 3 + [_vp, _sz, _vp, _vp, _vp, _sz, _vp]),
+    "rn50_distill_workspace_bytes": (_sz, [_i] * 3),
+    "distill_ce": (_i, [_i] * 3 + [_vp, _sz, _vp, _vp, _vp, _f, _f, _f, _vp, _vp, _sz, _vp, _sz, _vp]),
+    "distill_ce_bf16": (_i, [_i] * 3 + [_vp, _sz, _vp, _vp, _vp, _f, _f, _f, _vp, _vp, _sz, _vp, _sz, _vp]),
     "grad_pack_fp16": (_i, [_sz, _vp, _vp, _vp]),
     "grad_unpack_fp16": (_i, [_sz, _vp, _f, _vp, _vp]),
     "opt_update": (_i, [_sz, _vp, _vp, _vp, _vp, _vp, _vp, C.POINTER(OptHparams), _vp]),
@@ -389,6 +400,96 @@ def fc_bwd(n, j, k, f, w, dy, df, dw, db, stream=None):
 
 def softmax_ce(n, k, logits, labels, loss, dlogits, stream=None):
     _check(lib().softmax_ce(n, k, _ptr(logits), _ptr(labels), _ptr(loss), _ptr(dlogits), _stream(stream)))
+
+
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+TOPK_MAX = 256
+
+
+def _arg(t, dev, count, dtype):
+    """Pointer of a tensor (None: NULL) that has to hold at least `count` elements of `dtype` on the GPU `dev`, the current one, where the call launches."""
+    if t is None:
+        return None
+    assert t.get_device() == dev and t.is_contiguous() and t.dtype is dtype and t.numel() >= count, \
+        "wanted: a contiguous %s tensor of %d elements on the current GPU" % (dtype, count)
+    return t.data_ptr()
+
+
+def rn50_gn_workspace_bytes(n, c, h, w, groups):
+    return lib().rn50_gn_workspace_bytes(n, c, h, w, groups)
+
+
+def _gn_fwd(fn, dt, n, c, h, w, groups, x, gamma, beta, eps, residual, act, y, save_mean, save_invstd, ws, stream, layout):
+    f32, size, stats, dev = torch.float32, n * c * h * w, n * groups, torch.cuda.current_device()
+    _check(fn(n, c, h, w, layout, groups, _arg(x, dev, size, dt), _arg(gamma, dev, c, f32), _arg(beta, dev, c, f32), eps, _arg(residual, dev, size, dt), act,
+              _arg(y, dev, size, dt), _arg(save_mean, dev, stats, f32), _arg(save_invstd, dev, stats, f32), _ptr(ws), _bytes(ws), _stream(stream)))
+
+
+def gn_fwd(n, c, h, w, groups, x, gamma, beta, eps, residual, act, y, save_mean, save_invstd, ws, stream=None, layout=LAYOUT_NHWC):
+    _gn_fwd(lib().gn_fwd, torch.float32, n, c, h, w, groups, x, gamma, beta, eps, residual, act, y, save_mean, save_invstd, ws, stream, layout)
+
+
+def gn_fwd_bf16(n, c, h, w, groups, x, gamma, beta, eps, residual, act, y, save_mean, save_invstd, ws, stream=None, layout=LAYOUT_NHWC):
+    _gn_fwd(lib().gn_fwd_bf16, torch.bfloat16, n, c, h, w, groups, x, gamma, beta, eps, residual, act, y, save_mean, save_invstd, ws, stream, layout)
+
+
+def _gn_bwd(fn, dt, n, c, h, w, groups, x, dy, dy2, residual, gamma, beta, save_mean, save_invstd, act, dx, dresidual, dgamma, dbeta, ws, stream,
+            layout):
+    f32, size, stats, dev = torch.float32, n * c * h * w, n * groups, torch.cuda.current_device()
+    _check(fn(n, c, h, w, layout, groups, _arg(x, dev, size, dt), _arg(dy, dev, size, dt), _arg(dy2, dev, size, dt), _arg(residual, dev, size, dt),
+              _arg(gamma, dev, c, f32), _arg(beta, dev, c, f32), _arg(save_mean, dev, stats, f32), _arg(save_invstd, dev, stats, f32), act, _arg(dx, dev, size, dt),
+              _arg(dresidual, dev, size, dt), _arg(dgamma, dev, c, f32), _arg(dbeta, dev, c, f32), _ptr(ws), _bytes(ws), _stream(stream)))
+
+
+def gn_bwd(n, c, h, w, groups, x, dy, dy2, residual, gamma, beta, save_mean, save_invstd, act, dx, dresidual, dgamma, dbeta, ws, stream=None,
+           layout=LAYOUT_NHWC):
+    _gn_bwd(lib().gn_bwd, torch.float32, n, c, h, w, groups, x, dy, dy2, residual, gamma, beta, save_mean, save_invstd, act, dx, dresidual,
+            dgamma, dbeta, ws, stream, layout)
+
+
+def gn_bwd_bf16(n, c, h, w, groups, x, dy, dy2, residual, gamma, beta, save_mean, save_invstd, act, dx, dresidual, dgamma, dbeta, ws,
+                stream=None, layout=LAYOUT_NHWC):
+    _gn_bwd(lib().gn_bwd_bf16, torch.bfloat16, n, c, h, w, groups, x, dy, dy2, residual, gamma, beta, save_mean, save_invstd, act, dx, dresidual,
+            dgamma, dbeta, ws, stream, layout)
+
+
+def rn50_topk_workspace_bytes(n, k, t):
+    return lib().rn50_topk_workspace_bytes(n, k, t)
+
+
+def _topk(fn, dt, n, k, t, logits, ld, val, idx, ws, stream):
+    dev = torch.cuda.current_device()
+    _check(fn(n, k, t, _arg(logits, dev, (n - 1) * ld + k, dt), ld, _arg(val, dev, n * t, torch.float32), _arg(idx, dev, n * t, torch.int32), _ptr(ws),
+              _bytes(ws), _stream(stream)))
+
+
+def logits_topk(n, k, t, logits, ld, val, idx, ws, stream=None):
+    _topk(lib().logits_topk, torch.float32, n, k, t, logits, ld, val, idx, ws, stream)
+
+
+def logits_topk_bf16(n, k, t, logits, ld, val, idx, ws, stream=None):
+    _topk(lib().logits_topk_bf16, torch.bfloat16, n, k, t, logits, ld, val, idx, ws, stream)
+
+
+def rn50_distill_workspace_bytes(n, k, t):
+    return lib().rn50_distill_workspace_bytes(n, k, t)
+
+
+def _distill(fn, dt, n, k, t, logits, ld, labels, teacher_idx, teacher_val, alpha, tau, scale, loss, dlogits, ld_dlogits, ws, stream):
+    f32, i32, dev = torch.float32, torch.int32, torch.cuda.current_device()
+    _check(fn(n, k, t, _arg(logits, dev, (n - 1) * ld + k, dt), ld, _arg(labels, dev, n, i32), _arg(teacher_idx, dev, n * t, i32), _arg(teacher_val, dev, n * t, f32),
+              alpha, tau, scale, _arg(loss, dev, 3, f32), _arg(dlogits, dev, (n - 1) * ld_dlogits + k, dt), ld_dlogits, _ptr(ws), _bytes(ws),
+              _stream(stream)))
+
+
+def distill_ce(n, k, t, logits, ld, labels, teacher_idx, teacher_val, alpha, tau, scale, loss, dlogits, ld_dlogits, ws, stream=None):
+    _distill(lib().distill_ce, torch.float32, n, k, t, logits, ld, labels, teacher_idx, teacher_val, alpha, tau, scale, loss, dlogits, ld_dlogits,
+             ws, stream)
+
+
+def distill_ce_bf16(n, k, t, logits, ld, labels, teacher_idx, teacher_val, alpha, tau, scale, loss, dlogits, ld_dlogits, ws, stream=None):
+    _distill(lib().distill_ce_bf16, torch.bfloat16, n, k, t, logits, ld, labels, teacher_idx, teacher_val, alpha, tau, scale, loss, dlogits,
+             ld_dlogits, ws, stream)
 
 
 def grad_pack_fp16(count, g, out16, stream=None):

@@ -1,0 +1,100 @@
+"""What the group-normalization, top-logits and distillation calls refuse, before any HIP call (device pointers are stand-ins that
+are never followed)."""
+import numpy as np
+import pytest
+
+from paper_1711_04325_amd import binding as rn
+
+P = [4096 * (i + 1) for i in range(16)]   # distinct aligned addresses
+BIG = 1 << 40
+
+
+def _gn_fwd(L, n=2, c=8, h=3, w=5, layout=rn.LAYOUT_NHWC, groups=4, x=P[0], gamma=P[1], beta=P[2], eps=1e-5, res=P[3], act=1, y=P[4], mean=P[5],
+            inv=P[6], ws=P[7], nbytes=BIG, fn="gn_fwd"):
+    return getattr(L, fn)(n, c, h, w, layout, groups, x, gamma, beta, eps, res, act, y, mean, inv, ws, nbytes, None)
+
+
+def _gn_bwd(L, n=2, c=8, h=3, w=5, layout=rn.LAYOUT_NHWC, groups=4, x=P[0], dy=P[1], dy2=P[2], res=P[3], gamma=P[4], beta=P[5], mean=P[6], inv=P[7],
+            act=1, dx=P[8], dres=P[9], dgamma=P[10], dbeta=P[11], ws=P[12], nbytes=BIG, fn="gn_bwd"):
+    return getattr(L, fn)(n, c, h, w, layout, groups, x, dy, dy2, res, gamma, beta, mean, inv, act, dx, dres, dgamma, dbeta, ws, nbytes, None)
+
+
+GN_BOTH = [(dict(n=0), rn.EINVAL), (dict(h=-1), rn.EINVAL), (dict(groups=0), rn.EINVAL), (dict(groups=3), rn.EINVAL), (dict(groups=16), rn.EINVAL),
+           (dict(c=6, groups=2), rn.EUNSUPPORTED), (dict(layout=rn.LAYOUT_NCHW), rn.EUNSUPPORTED), (dict(act=3), rn.EINVAL), (dict(act=-1), rn.EINVAL),
+           (dict(x=None), rn.EINVAL), (dict(gamma=None), rn.EINVAL), (dict(beta=None), rn.EINVAL), (dict(ws=None), rn.EINVAL),
+           (dict(x=P[0] + 4), rn.EINVAL), (dict(res=P[3] + 8), rn.EINVAL), (dict(ws=P[7] + 2), rn.EINVAL), (dict(nbytes=0), rn.EWORKSPACE),
+           (dict(h=1 << 16, w=1 << 15), rn.EUNSUPPORTED), (dict(h=1 << 14, w=1 << 14), rn.EUNSUPPORTED), (dict(n=1 << 29), rn.EUNSUPPORTED)]
+
+
+@pytest.mark.parametrize("suffix", ["", "_bf16"])
+def test_group_norm_refusals(suffix):
+    L = rn.lib()
+    for args, code in GN_BOTH + [(dict(eps=-1.0), rn.EINVAL), (dict(eps=float("nan")), rn.EINVAL), (dict(y=None), rn.EINVAL), (dict(mean=None), rn.EINVAL),
+                                 (dict(inv=None), rn.EINVAL), (dict(y=P[0]), rn.EINVAL), (dict(y=P[3]), rn.EINVAL), (dict(inv=P[6] + 4), rn.EINVAL)]:
+        assert _gn_fwd(L, fn="gn_fwd" + suffix, **args) == code, args
+    for args, code in GN_BOTH + [(dict(dy=None), rn.EINVAL), (dict(dx=None), rn.EINVAL), (dict(dgamma=None), rn.EINVAL), (dict(mean=None), rn.EINVAL),
+                                 (dict(dx=P[0]), rn.EINVAL), (dict(dx=P[1]), rn.EINVAL), (dict(dx=P[9]), rn.EINVAL), (dict(dres=P[2]), rn.EINVAL),
+                                 (dict(dres=P[3]), rn.EINVAL), (dict(dy2=P[2] + 4), rn.EINVAL), (dict(dbeta=P[11] + 4), rn.EINVAL)]:
+        assert _gn_bwd(L, fn="gn_bwd" + suffix, **args) == code, args
+    assert b"gn_bwd" in L.rn50_last_error()
+
+
+def test_group_norm_workspace_query():
+    assert rn.rn50_gn_workspace_bytes(32, 64, 112, 112, 32) >= 2 * 4 * 32 * 64
+    for bad in ((0, 8, 3, 5, 4), (2, 6, 3, 5, 2), (2, 8, 3, 5, 3), (2, 8, 3, 5, 0), (2, 8, 1 << 16, 1 << 15, 4), (1 << 29, 8, 1, 1, 4)):
+        assert rn.rn50_gn_workspace_bytes(*bad) == 0, bad
+
+
+def _topk(L, n=3, k=10, t=4, z=P[0], ld=12, val=P[1], idx=P[2], ws=P[3], nbytes=BIG, fn="logits_topk"):
+    return getattr(L, fn)(n, k, t, z, ld, val, idx, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("suffix", ["", "_bf16"])
+def test_topk_refusals(suffix):
+    L = rn.lib()
+    for args, code in [(dict(n=0), rn.EINVAL), (dict(k=0), rn.EINVAL), (dict(t=0), rn.EINVAL), (dict(t=11), rn.EINVAL), (dict(ld=9), rn.EINVAL),
+                       (dict(k=1000, ld=1000, t=257), rn.EUNSUPPORTED), (dict(n=1 << 22), rn.EUNSUPPORTED), (dict(ld=1 << 31), rn.EINVAL),
+                       (dict(z=None), rn.EINVAL), (dict(val=None), rn.EINVAL), (dict(idx=None), rn.EINVAL), (dict(z=P[0] + 4), rn.EINVAL),
+                       (dict(val=P[1] + 8), rn.EINVAL), (dict(idx=P[2] + 4), rn.EINVAL), (dict(ws=P[3] + 4), rn.EINVAL)]:
+        assert _topk(L, fn="logits_topk" + suffix, **args) == code, args
+    need = rn.rn50_topk_workspace_bytes(1, 131072, 256)
+    if need:
+        args = dict(n=1, k=131072, ld=131072, t=256)
+        assert _topk(L, fn="logits_topk" + suffix, nbytes=need - 1, **args) == rn.EWORKSPACE
+        assert _topk(L, fn="logits_topk" + suffix, ws=None, nbytes=need, **args) == rn.EINVAL
+    for bad in ((0, 5, 1), (1, 0, 1), (1, 5, 0), (1, 5, 6)):
+        assert rn.rn50_topk_workspace_bytes(*bad) == 0, bad
+
+
+def _distill(L, n=3, k=10, t=4, z=P[0], ld=12, labels=P[1], idx=P[2], val=P[3], alpha=0.5, tau=2.0, scale=1.0, loss=P[4], dz=P[5], ldd=12, ws=P[6],
+             nbytes=BIG, fn="distill_ce"):
+    return getattr(L, fn)(n, k, t, z, ld, labels, idx, val, alpha, tau, scale, loss, dz, ldd, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("suffix", ["", "_bf16"])
+def test_distillation_refusals(suffix):
+    L = rn.lib()
+    nan, inf = float("nan"), float("inf")
+    for args, code in [(dict(n=0), rn.EINVAL), (dict(k=0), rn.EINVAL), (dict(t=0), rn.EINVAL), (dict(t=-1, alpha=0.0), rn.EINVAL),
+                       (dict(t=257), rn.EUNSUPPORTED), (dict(n=1 << 22), rn.EUNSUPPORTED), (dict(ld=9), rn.EINVAL), (dict(ldd=9), rn.EINVAL),
+                       (dict(ld=1 << 31), rn.EINVAL), (dict(ldd=1 << 31), rn.EINVAL), (dict(alpha=-0.1), rn.EINVAL), (dict(alpha=1.1), rn.EINVAL),
+                       (dict(alpha=nan), rn.EINVAL), (dict(tau=0.0), rn.EINVAL), (dict(tau=nan), rn.EINVAL), (dict(tau=2000.0), rn.EINVAL),
+                       (dict(tau=1e-4), rn.EINVAL), (dict(scale=nan), rn.EINVAL), (dict(scale=inf), rn.EINVAL), (dict(z=None), rn.EINVAL),
+                       (dict(labels=None), rn.EINVAL), (dict(idx=None), rn.EINVAL), (dict(val=None), rn.EINVAL), (dict(loss=None), rn.EINVAL),
+                       (dict(ws=None), rn.EINVAL), (dict(dz=P[0]), rn.EINVAL), (dict(nbytes=0), rn.EWORKSPACE)] + \
+                      [(dict([(name, P[8] + 4)]), rn.EINVAL) for name in ("z", "labels", "idx", "val", "loss", "dz", "ws")]:
+        assert _distill(L, fn="distill_ce" + suffix, **args) == code, args
+    need = rn.rn50_distill_workspace_bytes(3, 10, 4)
+    assert need > 0 and _distill(L, fn="distill_ce" + suffix, nbytes=need - 1) == rn.EWORKSPACE
+    for bad in ((0, 5, 1), (1, 0, 1), (1, 5, -1)):
+        assert rn.rn50_distill_workspace_bytes(*bad) == 0, bad
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    """Too few elements, another type or the CPU's memory: an assertion, no launch."""
+    import torch
+    x = torch.zeros(8)
+    with pytest.raises(AssertionError):
+        rn._arg(x, 0, 8, torch.float32)
+    assert rn._arg(None, 0, 8, torch.float32) is None
+    assert np.float32(rn.TOPK_MAX) == 256

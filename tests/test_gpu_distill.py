@@ -1,0 +1,343 @@
+"""GPU parity of the largest logits of a row and of the distillation loss, against the oracle.
+
+Tolerances of the loss count roundings of 2^-24.  A softmax value q = exp(d)/sum, d = z - max (divided by tau: one rounding more), has
+what d's roundings make of the exponential, |d| of them each, the exponential's own and the sum's, and the division: below 8 + 2|d|
+roundings of its size, and the sum 8 + 2 mean|d| (weighted with q).  A gradient is a difference of such numbers, each with its weight, and is rounded a few
+times itself; rounded to bf16 it is another 2^-8 of its value off, at most."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops as orc
+from paper_1711_04325_amd import binding as rn
+from tests.gpu_util import DEV, ws_bytes
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+# (n, k, t): one row and one class up to rows longer than a compute unit's registers, fewer rows than compute units and more, every
+# class kept, odd lengths
+SIZES = [(1, 1, 1), (1, 2, 2), (3, 7, 3), (5, 64, 10), (4, 1000, 10), (33, 1001, 64), (2, 5003, 256), (2, 40000, 17), (1, 131071, 100), (700, 33, 5),
+         (9, 256, 256), (257, 4099, 31), (3, 16384, 8), (1, 300001, 33), (2100, 130, 3)]
+
+
+def _padded(a, ld, dt, fill=float("nan")):
+    """The rows of a on the GPU, `ld` apart, `fill` between them, inside a larger buffer."""
+    n, k = a.shape
+    t = torch.full((n, ld), fill, dtype=dt)
+    t[:, :k] = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(dt)
+    return t.to(DEV)
+
+
+def _rows(seed, n, k, bf16, spread=3.0):
+    z = (np.random.default_rng(seed).normal(size=(n, k)) * spread).astype(np.float32)
+    return torch.from_numpy(z).to(torch.bfloat16).float().numpy() if bf16 else z
+
+
+def _topk(z, t, bf16, pad=0):
+    n, k = z.shape
+    dt = torch.bfloat16 if bf16 else torch.float32
+    val, idx = torch.full((n + 2, t), 7.0, device=DEV), torch.full((n + 2, t), 7, dtype=torch.int32, device=DEV)
+    # the padding holds what would win
+    (rn.logits_topk_bf16 if bf16 else rn.logits_topk)(n, k, t, _padded(z, k + pad, dt, float("inf")), k + pad, val, idx, ws_bytes(rn.rn50_topk_workspace_bytes(n, k, t)))
+    torch.cuda.synchronize()
+    assert (val[n:] == 7).all() and (idx[n:] == 7).all()
+    return val[:n].cpu().numpy(), idx[:n].cpu().numpy()
+
+
+def _check_topk(z, t, bf16, pad=0):
+    val, idx = _topk(z, t, bf16, pad)
+    rval, ridx = orc.topk(z, t)
+    np.testing.assert_array_equal(idx, ridx)
+    np.testing.assert_array_equal(val, rval.astype(np.float32))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("pad", [0, 5])
+@pytest.mark.parametrize("n,k,t", SIZES)
+def test_topk(n, k, t, pad, bf16):
+    _check_topk(_rows(n + k + t, n, k, bf16), t, bf16, pad)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n,k,t", [(3, 1000, 10), (2, 5003, 256), (2, 40000, 64), (1, 131071, 256), (4, 64, 64), (300, 2050, 200), (270, 20011, 256)])
+def test_topk_of_rows_that_are_hard_to_cut(n, k, t, bf16):
+    """Equal logits everywhere, few distinct ones, rising and falling rows, the largest side by side, one distinct value, all at the lowest
+    value, infinities and NaNs."""
+    g = np.random.default_rng(k)
+    falling = -np.arange(k, dtype=np.float32)
+    makers = [lambda: np.zeros((n, k)), lambda: g.integers(0, 3, (n, k)), lambda: np.tile(falling, (n, 1)), lambda: np.tile(falling[::-1], (n, 1)),
+              lambda: np.where(np.arange(k) // t == k // t // 2, 5.0 + g.random((n, k)), g.random((n, k))),
+              lambda: np.where(np.arange(k) == k - 1, 1.0, np.zeros((n, k))), lambda: np.full((n, k), -3.3e38),
+              lambda: np.where(g.random((n, k)) < 0.01, np.inf, np.where(g.random((n, k)) < 0.5, -np.inf, g.normal(size=(n, k)))),
+              lambda: np.where(g.random((n, k)) < 0.02, np.nan, np.where(g.random((n, k)) < 0.5, -0.0, 0.0)),
+              lambda: np.full((n, k), -np.inf), lambda: np.full((n, k), np.nan),
+              # the largest in one run of 64, 16 or 4 places, or all on one place in 64 or 1024
+              lambda: g.random((n, k)) + 10 * (np.arange(k) % 1024 < 64), lambda: g.random((n, k)) + 10 * (np.arange(k) % 4096 < 16),
+              lambda: g.random((n, k)) + 10 * (np.arange(k) % 64 == 3), lambda: g.random((n, k)) + 10 * (np.arange(k) % 1024 == 1023)]
+    for make in makers:
+        z = make().astype(np.float32)
+        z = torch.from_numpy(z).to(torch.bfloat16).float().numpy() if bf16 else z
+        _check_topk(z, t, bf16)
+
+
+def test_topk_far_into_memory():
+    """Rows that start beyond 2^31 elements."""
+    n, k, t, ld = 40, 70001, 9, 1 << 26
+    z = torch.zeros(((n - 1) * ld + k,), dtype=torch.bfloat16, device=DEV)
+    rows = torch.from_numpy(_rows(1, n, k, True)).to(torch.bfloat16).to(DEV)
+    for i in range(n):
+        z[i * ld:i * ld + k] = rows[i]
+    val, idx = torch.empty((n, t), device=DEV), torch.empty((n, t), dtype=torch.int32, device=DEV)
+    rn.logits_topk_bf16(n, k, t, z, ld, val, idx, ws_bytes(rn.rn50_topk_workspace_bytes(n, k, t)))
+    rval, ridx = orc.topk(rows.float().cpu().numpy(), t)
+    np.testing.assert_array_equal(idx.cpu().numpy(), ridx)
+    # the loss and its gradient on the same rows, in place of nothing: the gradient of the last row lies beyond 2^31 elements too
+    dz = torch.zeros_like(z)
+    loss = torch.empty(3, device=DEV)
+    labels = torch.arange(n, dtype=torch.int32, device=DEV)
+    rn.distill_ce_bf16(n, k, t, z, ld, labels, idx, val, 0.5, 2.0, 1.0, loss, dz, ld, ws_bytes(rn.rn50_distill_workspace_bytes(n, k, t)))
+    _, grad = orc.distill_ce(rows[-1:].double().cpu().numpy(), [n - 1], idx[-1:].cpu().numpy(), val[-1:].cpu().numpy(), 0.5, 2.0, 1.0)
+    got = dz[(n - 1) * ld:].double().cpu().numpy()
+    assert np.abs(got - grad[0]).max() <= 2.0 ** -8 * np.abs(grad).max() and (dz[k:ld] == 0).all()
+
+
+def _teacher(seed, z, t, few=True):
+    """Kept entries: distinct classes, some rows with fewer of them, one with none where there are enough."""
+    g = np.random.default_rng(seed)
+    n, k = z.shape
+    idx = np.stack([g.permutation(k)[:t] for _ in range(n)]).astype(np.int32)
+    val = (0.6 * np.take_along_axis(z, idx, 1) + 2 * g.normal(size=(n, t))).astype(np.float32)
+    if few:
+        for r in range(n):
+            if r % 5 == 1:
+                idx[r, g.random(t) < 0.5] = -1
+            if r % 5 == 2:
+                val[r, g.random(t) < 0.5] = -np.inf
+            if r % 5 == 3:
+                idx[r] = -1
+    return idx, val
+
+
+def _distill(z, labels, idx, val, alpha, tau, scale, bf16, pad=0, grad=True):
+    n, k = z.shape
+    t = 0 if idx is None else idx.shape[1]
+    dt = torch.bfloat16 if bf16 else torch.float32
+    i32 = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(DEV)
+    dz = torch.full((n + 2, k + pad), 55.0, dtype=dt, device=DEV)
+    loss = torch.full((8,), 55.0, device=DEV)
+    (rn.distill_ce_bf16 if bf16 else rn.distill_ce)(
+        n, k, t, _padded(z, k + pad, dt), k + pad, i32(labels), i32(idx), None if val is None else torch.from_numpy(val).to(DEV), alpha, tau, scale, loss,
+        dz if grad else None, k + pad, ws_bytes(rn.rn50_distill_workspace_bytes(n, k, t)))
+    torch.cuda.synchronize()
+    assert (loss[3:] == 55).all() and (dz[n:] == 55).all() and (dz[:, k:] == 55).all() and (grad or (dz == 55).all())
+    return loss[:3].double().cpu().numpy(), dz[:n, :k].double().cpu().numpy()
+
+
+def _bounds(z, labels, idx, val, alpha, tau, scale):
+    """What roundings may make of the three losses and of the gradient."""
+    z = z.astype(np.float64)
+    n, k = z.shape
+    d = np.where(np.isfinite(z), z - z.max(1, keepdims=True), 0)
+    off, parts = np.zeros((n, k)), np.zeros(2)
+
+    def softmax_off(x):
+        q = np.exp(x)
+        q /= q.sum(1, keepdims=True)
+        x = np.where(np.isfinite(x), x, 0)   # masked: q = 0
+        return q, q * (8 + 2 * np.abs(x)) + q * (8 + 2 * (q * np.abs(x)).sum(1, keepdims=True))
+
+    if labels is not None:
+        q, e = softmax_off(np.where(np.isfinite(z), d, -np.inf))
+        has = np.asarray(labels) != -1
+        one = np.zeros((n, k))
+        one[has.nonzero()[0], np.asarray(labels)[has]] = 1
+        off += (1 - alpha) * has[:, None] * (e + 4 * q + 4 * one)
+        lse = np.log(np.exp(d).sum(1))
+        parts[0] = ((8 + 4 * np.abs(lse) + 2 * np.abs(d[np.arange(n), np.where(has, labels, 0)])) * has).sum()
+    if idx is not None:
+        q, e = softmax_off(np.where(np.isfinite(z), d / tau, -np.inf))
+        keep = (idx != -1) & (val != -np.inf)
+        some = keep.any(1)
+        v = np.where(keep, val.astype(np.float64), -np.inf) / tau
+        v = np.where(some[:, None], v - np.where(some, v.max(1), 0)[:, None], -1.0)
+        p, pe = softmax_off(v)
+        fine = np.where(np.isfinite(v), v, 0)
+        p, pe = p * keep, (pe + 8 * p) * keep
+        off += alpha * tau * some[:, None] * (e + 6 * q)
+        for r in np.nonzero(some)[0]:
+            at = np.where(keep[r], idx[r], 0)
+            np.add.at(off[r], at, alpha * tau * (pe[r] + 6 * p[r]))
+            terms = np.abs(fine[r]) + np.abs(d[r, at] / tau) + np.abs(np.log(np.exp(d[r] / tau).sum())) + np.log(keep[r].sum() + 1)
+            parts[1] += tau * tau * ((p[r] * (24 + 6 * terms)).sum() + (pe[r] * terms).sum())
+    parts *= U * scale
+    return np.array([(1 - alpha) * parts[0] + alpha * parts[1], *parts]), off * U * scale
+
+
+def _check(z, labels, idx, val, alpha, tau, scale, bf16, pad=0):
+    loss, dz = _distill(z, labels, idx, val, alpha, tau, scale, bf16, pad)
+    rloss, rdz = orc.distill_ce(z, labels, idx, val, alpha, tau, scale)
+    loss_tol, off = _bounds(z, labels if alpha < 1 else None, idx if alpha > 0 else None, val, alpha, tau, scale)
+    if alpha == 1:
+        rloss[1] = 0
+    if alpha == 0:
+        rloss[2] = 0
+    assert (np.abs(loss - rloss) <= loss_tol + 4 * U * np.abs(rloss)).all(), (loss, rloss, loss_tol)
+    assert np.isfinite(dz).all()
+    over = np.abs(dz - rdz) - off - (2.0 ** -8 * np.abs(rdz) if bf16 else 0) - 1e-37
+    assert over.max() <= 0, (over.max(), np.unravel_index(over.argmax(), over.shape))
+    alone, _ = _distill(z, labels, idx, val, alpha, tau, scale, bf16, pad, grad=False)
+    assert (np.abs(alone - rloss) <= loss_tol + 4 * U * np.abs(rloss)).all()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("alpha,tau", [(0.25, 4.0), (0.5, 1.0), (1.0, 1.5), (0.0, 2.0), (1.0, 1.0)])
+@pytest.mark.parametrize("n,k,t", SIZES)
+def test_distillation(n, k, t, alpha, tau, bf16):
+    z = _rows(n * 3 + k + t, n, k, bf16)
+    idx, val = _teacher(n + k, z, t)
+    labels = np.random.default_rng(k).integers(0, k, n)
+    labels[4::7] = -1
+    _check(z, labels, idx, val, alpha, tau, 1 / n, bf16, pad=(0, 3, 64)[(n + k) % 3])
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n,k,t", [(6, 50, 12), (6, 3001, 256), (6, 70001, 40), (300, 1030, 20)])
+def test_distillation_with_masked_classes_and_repeated_ones(n, k, t, bf16):
+    """Classes masked by -infinity and by a very low value, a class kept several times, the label among the kept, logits far apart."""
+    g = np.random.default_rng(k)
+    z = _rows(k, n, k, bf16, 20.0)
+    idx, val = _teacher(k, z, t)
+    idx[0, 1:4] = idx[0, 0]
+    idx[4] = idx[4, 0]
+    labels = g.integers(0, k, n)
+    labels[0], labels[5] = idx[0, 0], -1
+    masked = g.random((n, k)) < 0.3
+    for r in range(n):
+        masked[r, labels[r]] = masked[r, np.maximum(idx[r], 0)] = False
+    for low in (-np.inf, -3.3e38):
+        zm = np.where(masked, np.float32(low), z).astype(np.float32)
+        zm = torch.from_numpy(zm).to(torch.bfloat16).float().numpy() if bf16 else zm
+        _check(zm, labels, idx, val, 0.3, 2.0, 1.0, bf16)
+        _, dz = _distill(zm, labels, idx, val, 0.3, 2.0, 1.0, bf16)
+        assert (dz[masked] == 0).all()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("n,k", [(8, 40), (8, 2500), (8, 90001), (300, 1030)])
+def test_distillation_of_bad_rows(n, k, bf16):
+    """What makes the loss NaN or infinite, and that it stays in its row's gradient."""
+    t = 4
+    z = _rows(k, n, k, bf16)
+    idx, val = _teacher(k, z, t, few=False)
+    labels = np.arange(n) % 5
+    run = lambda z=z, labels=labels, idx=idx, val=val: _distill(z, labels, idx, val, 0.5, 2.0, 1.0, bf16)
+    _, clean = run()
+    rest = [r for r in range(n) if r != 3]
+    for bad in (k, -2, 2 ** 31 - 1, -2 ** 31):
+        lab, ind = labels.copy(), idx.copy()
+        lab[3], ind[3, 2] = bad, bad
+        loss, dz = run(labels=lab)
+        assert np.isnan(loss[0]) and np.isnan(loss[1]) and np.isfinite(loss[2]) and np.array_equal(dz[rest], clean[rest]) and np.isfinite(dz[3]).all()
+        loss, dz = run(idx=ind)
+        assert np.isnan(loss[0]) and np.isfinite(loss[1]) and np.isnan(loss[2]) and np.array_equal(dz[rest], clean[rest]) and np.isfinite(dz[3]).all()
+    for value in (np.nan, np.inf):
+        zz = z.copy()
+        zz[3, k // 2] = value
+        loss, dz = run(z=zz)
+        assert np.isnan(loss).all() and np.isnan(dz[3]).all() and np.array_equal(dz[rest], clean[rest])
+    zz = z.copy()
+    zz[3] = -np.inf
+    loss, dz = run(z=zz)
+    assert np.isnan(loss).all() and np.isnan(dz[3]).all() and np.array_equal(dz[rest], clean[rest])
+    zz = z.copy()
+    zz[3, labels[3]] = -np.inf
+    idx2 = idx.copy()
+    idx2[3] = [c for c in range(k - 1, k - 6, -1) if c != labels[3]][:t]
+    loss, dz = run(z=zz, idx=idx2)
+    assert np.isposinf(loss[0]) and np.isposinf(loss[1]) and np.isfinite(loss[2]) and np.isfinite(dz).all()
+    zz = z.copy()
+    zz[3, idx[3, 1]] = -np.inf
+    lab = labels.copy()
+    lab[3] = -1
+    loss, dz = run(z=zz, labels=lab)
+    assert np.isposinf(loss[0]) and np.isfinite(loss[1]) and np.isposinf(loss[2]) and np.isfinite(dz).all()
+    # a row that counts for nothing is not looked at
+    zz, lab, ind = z.copy(), labels.copy(), idx.copy()
+    zz[3], lab[3], ind[3] = np.nan, -1, -1
+    loss, dz = run(z=zz, labels=lab, idx=ind)
+    assert np.isfinite(loss).all() and (dz[3] == 0).all() and np.array_equal(dz[rest], clean[rest])
+    # a term without weight does not count, however bad
+    lab, ind = np.full(n, -9), np.full((n, t), -9, np.int32)
+    loss, dz = _distill(z, lab, idx, val, 1.0, 2.0, 1.0, bf16)
+    assert np.isfinite(loss).all() and loss[1] == 0 and np.isfinite(dz).all()
+    loss, dz = _distill(z, labels, ind, val, 0.0, 2.0, 1.0, bf16)
+    assert np.isfinite(loss).all() and loss[2] == 0 and np.isfinite(dz).all()
+    # teachers and labels left out
+    for args in ((None, idx, val, 1.0), (labels, None, None, 0.0)):
+        loss, dz = _distill(z, *args, 2.0, 1.0, bf16)
+        ref = _distill(z, labels, idx, val, args[3], 2.0, 1.0, bf16)
+        assert np.array_equal(loss, ref[0]) and np.array_equal(dz, ref[1])
+
+
+def test_gradient_against_differences():
+    """Central differences of the call's own loss, of a row small enough for fp32 to show them: a loss of 8 at most has a rounding of 2^-22,
+    a step of 2^-5 (exact) makes that 8e-6 of the difference quotient; the third derivative, below 1/tau^2 <= 1, a sixth of the step's square
+    1.7e-4."""
+    g = np.random.default_rng(3)
+    k, t, step = 6, 3, 2.0 ** -5
+    z = (np.round(g.normal(size=(1, k)) * 64) / 64).astype(np.float32)
+    idx, val = np.array([[4, 0, 2]], np.int32), g.normal(size=(1, t)).astype(np.float32)
+    labels = np.array([2])
+    _, dz = _distill(z, labels, idx, val, 0.5, 2.0, 1.0, False)
+    for i in range(k):
+        e = np.zeros_like(z)
+        e[0, i] = step
+        hi, lo = (_distill(z + s * e, labels, idx, val, 0.5, 2.0, 1.0, False, grad=False)[0][0] for s in (1, -1))
+        assert abs((hi - lo) / (2 * step) - dz[0, i]) <= 1.7e-4 + 1e-5
+
+
+@pytest.mark.parametrize("n,k,t", [(32, 1000, 10), (300, 9000, 64), (2, 131071, 100)])
+def test_streams_and_graphs(n, k, t):
+    """A teacher's logits picked and learned from: two streams at once, and a captured pair replayed on other inputs, give the bits of a
+    call by itself."""
+    def make(seed):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        s = {"teacher": torch.randn((n, k), generator=g, device=DEV), "z": torch.randn((n, k), generator=g, device=DEV),
+             "labels": torch.randint(0, k, (n,), generator=g, device=DEV, dtype=torch.int32)}
+        s.update(val=torch.zeros((n, t), device=DEV), idx=torch.zeros((n, t), dtype=torch.int32, device=DEV), loss=torch.zeros(3, device=DEV),
+                 dz=torch.zeros((n, k), device=DEV), ws=ws_bytes(rn.rn50_topk_workspace_bytes(n, k, t)), ws2=ws_bytes(rn.rn50_distill_workspace_bytes(n, k, t)))
+        return s
+
+    def run(s):
+        rn.logits_topk(n, k, t, s["teacher"], k, s["val"], s["idx"], s["ws"])
+        rn.distill_ce(n, k, t, s["z"], k, s["labels"], s["idx"], s["val"], 0.5, 2.0, 1 / n, s["loss"], s["dz"], k, s["ws2"])
+        return [s[key] for key in ("val", "idx", "loss", "dz")]
+
+    sets = [make(i) for i in range(2)]
+    want = [[o.clone() for o in run(s)] for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(3):
+        for s, st in zip(sets, streams):
+            with torch.cuda.stream(st):
+                run(s)
+    torch.cuda.synchronize()
+    for s, ref in zip(sets, want):
+        for key, r in zip(("val", "idx", "loss", "dz"), ref):
+            assert torch.equal(s[key], r), key
+    s = sets[0]
+    first = {key: s[key].clone() for key in ("teacher", "z", "labels")}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run(s)
+    for i in (1, 0, 1, 0):
+        for key in first:
+            s[key].copy_(first[key] if i == 0 else sets[1][key])
+        for o in out:
+            o.fill_(3)
+        s["ws"].fill_(255)
+        s["ws2"].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        for o, r in zip(out, want[i]):
+            assert torch.equal(o, r)

@@ -1,0 +1,300 @@
+"""GPU parity of group normalization against the oracle, forward and backward, in fp32 and with bf16 tensors.
+
+Tolerances count roundings of 2^-24 against the numbers that are rounded.  u = (x - mean)*(gamma*invstd) + beta + residual has five, of
+numbers no larger than Y = |gamma|*invstd*(|x - mean| + M) + |beta| + |residual|, where M, the group's mean |x|, bounds what mean is off by
+in units of a rounding (a sum of pairs of pairs ... of short runs: a few roundings of its size); 1/sqrt and the sum of squares behind it
+add a few relative to Y: below 16 of them, 1e-6 Y.  dx = invstd*(gamma*dz - A - xhat*B) likewise with D = invstd*(|gamma*dz| + a + |xhat|*b),
+a and b the group's means of |gamma*dz| and |gamma*dz*xhat|.  SiLU's value and slope have an exponential (2 roundings), a division and
+five roundings more, of numbers below 1.1 |u| and 1.1 (1 + |u|).  dgamma and dbeta: sums of terms t with these errors each, so 1e-6
+sum|t|.  bf16 outputs: half a step more, 2^-8 of the value."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops as orc
+from paper_1711_04325_amd import binding as rn
+from tests.gpu_util import DEV, ws_bytes
+
+pytestmark = pytest.mark.gpu
+
+ACTS = {"none": rn.ACT_NONE, "relu": rn.ACT_RELU, "silu": rn.ACT_SILU}
+EPS = 1e-5
+# (n, c, h, w, groups): one value to a group up to many, groups of 1, 2, 3, 5, 8, 10, 24, 64 channels and all of them, one pixel, odd
+# images, images of more pixels than any workgroup holds, more images than compute units
+SHAPES = [(1, 4, 1, 1, 1), (2, 8, 1, 1, 8), (1, 4, 1, 3, 2), (3, 24, 5, 7, 8), (2, 20, 9, 4, 4), (2, 64, 56, 56, 32), (2, 2048, 7, 7, 32), (4, 256, 14, 14, 32),
+          (1, 320, 33, 35, 32), (5, 48, 13, 11, 2), (1, 64, 112, 112, 32), (2, 12, 130, 67, 12), (300, 16, 3, 3, 4), (1, 8, 257, 255, 1), (2, 1028, 3, 3, 4),
+          (7, 512, 4, 4, 1), (1, 4, 1, 1, 4), (2, 256, 40, 40, 4)]
+
+
+def _round(a, bf16):
+    t = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32))
+    return (t.to(torch.bfloat16).float() if bf16 else t).numpy()
+
+
+def _inputs(seed, shape, bf16, act, use_res, mean=1.0):
+    """fp32 arrays, rounded to bf16 where the call takes such; no pre-activation within 1e-3 of the ReLU's corner."""
+    n, c, h, w, groups = shape
+    g = np.random.default_rng(seed)
+    x = g.normal(size=(n, c, h, w)) * g.uniform(0.5, 2.0, size=(1, c, 1, 1)) + mean * g.uniform(-1, 1, size=(1, c, 1, 1))
+    gamma, beta = _round(1 + 0.2 * g.normal(size=c), False), _round(0.3 * g.normal(size=c), False)
+    x, res, dy, dy2 = (_round(v, bf16) for v in (x, *g.normal(size=(3, n, c, h, w))))
+    if not use_res:
+        res = None
+    if act == "relu":
+        for _ in range(3):   # moved off it (which moves the statistics a little)
+            u = orc.gn_fwd(x, groups, gamma, beta, EPS, res)[0]
+            near = np.abs(u) < 2e-3
+            if use_res:
+                res = np.where(near, _round(res + np.where(u < 0, -0.03, 0.03) * (1 + np.abs(res)), bf16), res)
+            elif h * w * (c // groups) > 2:
+                x = np.where(near, _round(x + np.where(u < 0, -0.03, 0.03) * (1 + np.abs(x)), bf16), x)
+            else:
+                beta = beta + np.float32(0.05)
+    return x.astype(np.float32), gamma, beta, None if res is None else res.astype(np.float32), dy, dy2
+
+
+def _dev(a, dt):
+    if a is None:
+        return None
+    t = torch.from_numpy(np.ascontiguousarray(np.transpose(a, (0, 2, 3, 1)) if a.ndim == 4 else a, dtype=np.float32))
+    return (t.to(dt) if a.ndim == 4 else t).to(DEV)
+
+
+def _host(t):
+    a = t.double().cpu().numpy()
+    return np.transpose(a, (0, 3, 1, 2)) if a.ndim == 4 else a
+
+
+def _room(shape, dt):
+    """A tensor of the shape inside a larger one whose other values have to stay; (tensor, check)."""
+    size = int(np.prod(shape))
+    whole = torch.full((size + 512,), 77.0, dtype=dt, device=DEV)
+
+    def untouched():
+        return bool((whole[:256] == 77).all()) and bool((whole[256 + size:] == 77).all())
+
+    return whole[256:256 + size].view(shape), untouched
+
+
+def _fwd(shape, x, gamma, beta, res, act, bf16, stats=True):
+    n, c, h, w, groups = shape
+    dt = torch.bfloat16 if bf16 else torch.float32
+    (y, ok_y), (mean, ok_m), (inv, ok_i) = _room((n, h, w, c), dt), _room((n, groups), torch.float32), _room((n, groups), torch.float32)
+    call = rn.gn_fwd_bf16 if bf16 else rn.gn_fwd
+    call(n, c, h, w, groups, _dev(x, dt), _dev(gamma, dt), _dev(beta, dt), EPS, _dev(res, dt), ACTS[act], y, mean if stats else None,
+         inv if stats else None, ws_bytes(rn.rn50_gn_workspace_bytes(n, c, h, w, groups)))
+    torch.cuda.synchronize()
+    assert ok_y() and ok_m() and ok_i()
+    return y, mean, inv
+
+
+def _bwd(shape, x, dy, dy2, res, gamma, beta, mean, inv, act, bf16, want_dres):
+    n, c, h, w, groups = shape
+    dt = torch.bfloat16 if bf16 else torch.float32
+    (dx, ok1), (dres, ok2), (dg, ok3), (db, ok4) = _room((n, h, w, c), dt), _room((n, h, w, c), dt), _room((c,), torch.float32), _room((c,), torch.float32)
+    call = rn.gn_bwd_bf16 if bf16 else rn.gn_bwd
+    call(n, c, h, w, groups, _dev(x, dt), _dev(dy, dt), _dev(dy2, dt), _dev(res, dt), _dev(gamma, dt), _dev(beta, dt), _dev(mean, dt), _dev(inv, dt),
+         ACTS[act], dx, dres if want_dres else None, dg, db, ws_bytes(rn.rn50_gn_workspace_bytes(n, c, h, w, groups)))
+    torch.cuda.synchronize()
+    assert ok1() and ok2() and ok3() and ok4()
+    return dx, dres, dg, db
+
+
+def _within(got, ref, tol, what):
+    got = _host(got)
+    assert np.isfinite(got).all(), what
+    over = np.abs(got - ref) / np.maximum(tol, 1e-300)
+    assert over.max() <= 1, (what, float(over.max()))
+
+
+def _by_group(v, groups, c):
+    """The group's mean of v at every channel."""
+    n = v.shape[0]
+    return np.repeat(v.reshape(n, groups, -1).mean(axis=2), c // groups, axis=1)[:, :, None, None]
+
+
+HALF = 2.0 ** -8   # half a step of bf16
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("act,use_res", [("none", False), ("relu", True), ("silu", False), ("silu", True), ("relu", False)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_gn_fwd(shape, act, use_res, bf16):
+    n, c, h, w, groups = shape
+    x, gamma, beta, res, _, _ = _inputs(sum(shape) + 3 * use_res, shape, bf16, act, use_res)
+    y, mean, inv = _fwd(shape, x, gamma, beta, res, act, bf16)
+    ry, rmean, rinv = orc.gn_fwd(x, groups, gamma, beta, EPS, res, act)
+    M = _by_group(np.abs(x.astype(np.float64)), groups, c)
+    up = lambda s: np.repeat(s, c // groups, axis=1)[:, :, None, None]
+    ch = lambda v: np.abs(v.astype(np.float64))[None, :, None, None]
+    Y = ch(gamma) * up(rinv) * (np.abs(x - up(rmean)) + M) + ch(beta) + (np.abs(res) if use_res else 0)
+    _within(mean, rmean, 1e-6 * M[:, ::c // groups, 0, 0], "mean")
+    # invstd: what mean is off by enters squared where the variance is not small beside it
+    _within(inv, rinv, 1e-6 * rinv * (1 + (1e-6 * M[:, ::c // groups, 0, 0] * rinv) ** 2 * 1e6), "invstd")
+    _within(y, ry, 1e-6 * Y * (1.2 if act == "silu" else 1) + (HALF * np.abs(ry) if bf16 else 0), "y")
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("act,use_res,use_dy2", [("none", False, False), ("relu", True, True), ("silu", False, False), ("relu", False, False),
+                                                 ("silu", True, False), ("none", True, True)])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_gn_bwd(shape, act, use_res, use_dy2, bf16):
+    n, c, h, w, groups = shape
+    x, gamma, beta, res, dy, dy2 = _inputs(7 + sum(shape) + 3 * use_res, shape, bf16, act, use_res)
+    _, mean, inv = orc.gn_fwd(x, groups, gamma, beta, EPS, res, act)
+    mean, inv = mean.astype(np.float32), inv.astype(np.float32)   # the same fp32 statistics on both sides
+    total = dy.astype(np.float64) + (dy2 if use_dy2 else 0)
+    rdx, rdz, rdg, rdb = orc.gn_bwd(x, total, groups, gamma, beta, mean, inv, res, act)
+    dx, dres, dg, db = _bwd(shape, x, dy, dy2 if use_dy2 else None, res, gamma, beta, mean, inv, act, bf16, use_res)
+    up = lambda s: np.repeat(s.astype(np.float64), c // groups, axis=1)[:, :, None, None]
+    ch = lambda v: np.abs(v.astype(np.float64))[None, :, None, None]
+    xhat = (x - up(mean)) * up(inv)
+    Y = ch(gamma) * np.abs(xhat) + ch(beta) + (np.abs(res) if use_res else 0)
+    # dz: a rounding where two gradients arrive, the slope's where it is smooth (it moves by up to 0.5 for what u is off by)
+    Z = (np.abs(dy) + (np.abs(dy2) if use_dy2 else 0)).astype(np.float64) * (1 + (1.1 * np.abs(Y) if act == "silu" else 0))
+    a = ch(gamma) * Z
+    D = up(inv) * (a + _by_group(a, groups, c) + np.abs(xhat) * _by_group(a * np.abs(xhat), groups, c))
+    _within(dx, rdx, 1e-6 * D + (HALF * np.abs(rdx) if bf16 else 0), "dx")
+    if use_res:
+        _within(dres, rdz, 1e-6 * Z + (HALF * np.abs(rdz) if bf16 else 0), "dresidual")
+    _within(dg, rdg, 1e-6 * (Z * (np.abs(xhat) + 1e-3)).sum(axis=(0, 2, 3)), "dgamma")
+    _within(db, rdb, 1e-6 * Z.sum(axis=(0, 2, 3)), "dbeta")
+
+
+@pytest.mark.parametrize("shape", [(2, 8, 33, 31, 2), (1, 64, 112, 112, 32), (1, 8, 257, 255, 1)])
+def test_gn_far_from_zero(shape):
+    """|mean| of 1000 standard deviations: sums of squares less the mean's square would lose the variance.  The mean's own rounding of
+    2^-24 * 1000 sigma is what is left, in y as in the bound Y."""
+    n, c, h, w, groups = shape
+    g = np.random.default_rng(1)
+    x = (0.1 * g.normal(size=(n, c, h, w)) + 100).astype(np.float32)
+    one, zero = np.ones(c, np.float32), np.zeros(c, np.float32)
+    y, mean, inv = _fwd(shape, x, one, zero, None, "none", False)
+    ry, rmean, rinv = orc.gn_fwd(x, groups, one, zero, EPS)
+    _within(mean, rmean, 1e-6 * rmean, "mean")
+    _within(inv, rinv, 1e-5 * rinv, "invstd")   # (1e-6 * 1000)^2 of the variance from the mean, 16 roundings: 2.0e-6 of it
+    _within(y, ry, 1e-6 * 10 * 100 + 1e-5 * np.abs(ry), "y")
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_gn_constant_groups_and_bad_values(bf16):
+    """A group without variance gives beta; a NaN or an infinity stays in its group."""
+    shape = (2, 8, 5, 3, 4)
+    x, gamma, beta, res, dy, _ = _inputs(3, shape, bf16, "none", False)
+    x[0, 0:2], x[0, 3, 1, 1], x[1, 6, 2, 2], x[1, 0, 0, 0] = 1.5, np.nan, np.inf, -np.inf
+    for act in ("none", "relu", "silu"):
+        y, mean, inv = (_host(t) for t in _fwd(shape, x, gamma, beta, None, act, bf16))
+        bad = np.zeros((2, 8), bool)
+        bad[0, 2:4] = bad[1, 6:8] = bad[1, 0:2] = True
+        assert np.isnan(y[bad]).all() and np.isfinite(y[~bad]).all()
+        if act == "none":
+            want = np.broadcast_to(_round(beta, bf16)[:2, None, None], (2, 5, 3))
+            assert np.array_equal(y[0, :2], want) and mean[0, 0] == 1.5
+            np.testing.assert_allclose(inv[0, 0], 1 / np.sqrt(EPS), rtol=1e-6)
+    clean = np.where(np.isfinite(x), x, 0).astype(np.float32)
+    _, mean, inv = orc.gn_fwd(clean, 4, gamma, beta, EPS)
+    dx, _, dg, db = (_host(t) for t in _bwd(shape, x, dy, None, None, gamma, beta, mean.astype(np.float32), inv.astype(np.float32), "silu", bf16, False))
+    assert np.isnan(dx[bad]).all() and np.isfinite(dx[~bad]).all()
+    assert np.isfinite(dg[[4, 5]]).all() and np.isnan(dg[[3, 6]]).all()
+
+
+def test_gn_without_statistics_and_unneeded_residual():
+    """Statistics left out change nothing; the backward pass without an activation does not look at the residual."""
+    shape = (3, 24, 5, 7, 8)
+    x, gamma, beta, res, dy, _ = _inputs(11, shape, False, "none", True)
+    a, mean, inv = _fwd(shape, x, gamma, beta, res, "none", False)
+    b, _, _ = _fwd(shape, x, gamma, beta, res, "none", False, stats=False)
+    assert torch.equal(a, b)
+    mean, inv = mean.cpu().numpy(), inv.cpu().numpy()
+    for p, q in zip(_bwd(shape, x, dy, None, res, gamma, beta, mean, inv, "none", False, True),
+                    _bwd(shape, x, dy, None, None, gamma, beta, mean, inv, "none", False, True)):
+        assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("shape", [(2, 64, 56, 56, 32), (1, 320, 33, 35, 32), (1, 8, 257, 255, 1), (300, 16, 3, 3, 4)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_gn_backward_takes_the_forwards_relu_decision(shape, bf16):
+    """With a constant dy of 1 and no residual, dz is the mask: it has to be [y > 0] of the forward pass for every element, those within
+    rounding of the corner among them."""
+    n, c, h, w, groups = shape
+    x, gamma, beta, res, _, _ = _inputs(5, shape, bf16, "none", True)
+    res = np.where(np.random.default_rng(2).random(res.shape) < 0.5, -_round(orc.gn_fwd(x, groups, gamma, beta, EPS)[0], bf16), res).astype(np.float32)
+    y, mean, inv = _fwd(shape, x, gamma, beta, res, "relu", bf16)
+    assert bf16 or int(((y > 0) & (y < 1e-6)).sum()) > 0
+    _, dz, _, _ = _bwd(shape, x, np.ones_like(x), None, res, gamma, beta, mean.cpu().numpy(), inv.cpu().numpy(), "relu", bf16, True)
+    assert torch.equal(dz > 0, y > 0)
+
+
+def _tensors(shape, bf16, seed):
+    n, c, h, w, groups = shape
+    dt = torch.bfloat16 if bf16 else torch.float32
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    r = lambda *s: torch.randn(s, generator=g, device=DEV)
+    e = lambda *s, t=torch.float32: torch.zeros(s, dtype=t, device=DEV)
+    return {"x": r(n, h, w, c).to(dt), "dy": r(n, h, w, c).to(dt), "gamma": 1 + 0.1 * r(c), "beta": r(c), "y": e(n, h, w, c, t=dt), "dx": e(n, h, w, c, t=dt),
+            "mean": e(n, groups), "inv": e(n, groups), "dg": e(c), "db": e(c), "ws": ws_bytes(rn.rn50_gn_workspace_bytes(n, c, h, w, groups))}
+
+
+def _both(shape, bf16, s):
+    n, c, h, w, groups = shape
+    fwd, bwd = (rn.gn_fwd_bf16, rn.gn_bwd_bf16) if bf16 else (rn.gn_fwd, rn.gn_bwd)
+    fwd(n, c, h, w, groups, s["x"], s["gamma"], s["beta"], EPS, None, rn.ACT_SILU, s["y"], s["mean"], s["inv"], s["ws"])
+    bwd(n, c, h, w, groups, s["x"], s["dy"], None, None, s["gamma"], s["beta"], s["mean"], s["inv"], rn.ACT_SILU, s["dx"], None, s["dg"], s["db"], s["ws"])
+    return [s[k] for k in ("y", "mean", "inv", "dx", "dg", "db")]
+
+
+@pytest.mark.parametrize("shape", [(2, 64, 56, 56, 32), (1, 320, 33, 35, 32), (1, 8, 257, 255, 1)])
+def test_gn_on_streams_and_in_graphs(shape):
+    """Two calls at once on streams of their own, and a captured pair replayed with other inputs: the bits of a call by itself."""
+    sets = [_tensors(shape, False, i) for i in range(2)]
+    want = [[t.clone() for t in _both(shape, False, s)] for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(3):
+        for s, st in zip(sets, streams):
+            with torch.cuda.stream(st):
+                _both(shape, False, s)
+    torch.cuda.synchronize()
+    for s, ref in zip(sets, want):
+        for k, r in zip(("y", "mean", "inv", "dx", "dg", "db"), ref):
+            assert torch.equal(s[k], r), k
+    s = sets[0]
+    first = {k: s[k].clone() for k in ("x", "dy", "gamma", "beta")}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _both(shape, False, s)
+    for i in (1, 0, 1, 0):
+        for k in first:
+            s[k].copy_(first[k] if i == 0 else sets[1][k])
+        for t in out:
+            t.fill_(9.0)
+        s["ws"].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, r in zip(out, want[i]):
+            assert torch.equal(t, r)
+
+
+def test_gn_more_than_2_to_31_elements():
+    """Offsets beyond 32 bits: the last images of a tensor of 2.2e9 elements are normalised as they are alone."""
+    n, c, h, w, groups = 34, 16, 2048, 2000, 4
+    one = torch.randn((1, h, w, c), device=DEV, generator=torch.Generator(device=DEV).manual_seed(4)).to(torch.bfloat16)
+    x = torch.empty((n, h, w, c), dtype=torch.bfloat16, device=DEV)
+    for i in range(n):
+        torch.mul(one[0], 1.0 + i % 3, out=x[i])
+    gamma, beta = torch.ones(c, device=DEV), torch.zeros(c, device=DEV)
+    y, dx, dy = torch.empty_like(x), torch.empty_like(x), x.roll(1, 3)
+    stats, dg, db = (torch.empty((n, groups), device=DEV), torch.empty((n, groups), device=DEV)), torch.empty(c, device=DEV), torch.empty(c, device=DEV)
+    ws = ws_bytes(rn.rn50_gn_workspace_bytes(n, c, h, w, groups))
+    rn.gn_fwd_bf16(n, c, h, w, groups, x, gamma, beta, EPS, None, rn.ACT_NONE, y, *stats, ws)
+    rn.gn_bwd_bf16(n, c, h, w, groups, x, dy, None, None, gamma, beta, *stats, rn.ACT_NONE, dx, None, dg, db, ws)
+    for i in (0, 16, 33):
+        y1, dx1, m1, i1 = torch.empty_like(one), torch.empty_like(one), torch.empty((1, groups), device=DEV), torch.empty((1, groups), device=DEV)
+        xi = x[i:i + 1].clone()
+        ws1 = ws_bytes(rn.rn50_gn_workspace_bytes(1, c, h, w, groups))
+        rn.gn_fwd_bf16(1, c, h, w, groups, xi, gamma, beta, EPS, None, rn.ACT_NONE, y1, m1, i1, ws1)
+        rn.gn_bwd_bf16(1, c, h, w, groups, xi, xi.roll(1, 3), None, None, gamma, beta, m1, i1, rn.ACT_NONE, dx1, None, dg.clone(), db.clone(), ws1)
+        # two cuts of an image round their sums apart: 2^-8 of a value and a step of the statistics
+        torch.testing.assert_close(stats[0][i], m1[0], rtol=1e-5, atol=1e-6)
+        torch.testing.assert_close(y[i].float(), y1[0].float(), rtol=2.0 ** -7, atol=1e-5)
+        torch.testing.assert_close(dx[i].float(), dx1[0].float(), rtol=2.0 ** -7, atol=1e-4)
