@@ -13,10 +13,20 @@ namespace rn50 {
 
 // ---- vectors of V channels of a row, as they lie in memory -----------------------------------------------------------------
 template <class T, int V> struct GnVec;
+template <> struct GnVec<float, 1> {
+    typedef float Raw;
+    static __device__ void unpack(Raw r, float *f) { f[0] = r; }
+    static __device__ Raw pack(const float *f) { return f[0]; }
+};
 template <> struct GnVec<float, 4> {
     typedef float4 Raw;
     static __device__ void unpack(const Raw &r, float *f) { f[0] = r.x; f[1] = r.y; f[2] = r.z; f[3] = r.w; }
     static __device__ Raw pack(const float *f) { return make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <> struct GnVec<bf16_t, 1> {
+    typedef bf16_t Raw;
+    static __device__ void unpack(Raw r, float *f) { f[0] = bf16_lo(r); }
+    static __device__ Raw pack(const float *f) { return (bf16_t)bf16_rne(f[0]); }
 };
 template <> struct GnVec<bf16_t, 4> {
     typedef uint2 Raw;
@@ -39,8 +49,9 @@ template <class T, int V> __device__ inline typename GnVec<T, V>::Raw gn_load(co
 template <class T, int V> __device__ inline void gn_store(T *p, const float *f) { *reinterpret_cast<typename GnVec<T, V>::Raw *>(p) = GnVec<T, V>::pack(f); }
 template <int V> __device__ inline void gn_load_floats(const float *p, float *f)
 {
+    constexpr int S = V == 1 ? 1 : 4;
 #pragma unroll
-    for (int v = 0; v < V; v += 4) GnVec<float, 4>::unpack(reinterpret_cast<const float4 *>(p)[v / 4], f + v);
+    for (int v = 0; v < V; v += S) GnVec<float, S>::unpack(gn_load<float, S>(p + v), f + v);
 }
 
 // ---- the activation --------------------------------------------------------------------------------------------------------
@@ -119,12 +130,12 @@ template <int V> __device__ inline void gn_wave_rows_sum(const GnMap &m, const G
         }
 }
 // Leaves the workgroup's sums of a thread's V values by column in out[W], W = cols*V (part: slots * W floats); threads beyond the
-// active ones bring zeros.  Ends with a barrier.
+// active ones bring zeros, or hold columns that nobody reads.  Ends with a barrier.
 template <int V> __device__ inline void gn_column_sums(const GnMap &m, const GnThread &t, float *v, float *part, float *out)
 {
     const int W = m.cols * V;
     gn_wave_rows_sum<V>(m, t, v);
-    if (t.active && t.lane_row == 0)
+    if (t.slot < m.slots && t.lane_row == 0)
 #pragma unroll
         for (int i = 0; i < V; ++i) part[t.slot * W + t.col * V + i] = v[i];
     __syncthreads();
@@ -135,23 +146,27 @@ template <int V> __device__ inline void gn_column_sums(const GnMap &m, const GnT
     }
     __syncthreads();
 }
-// Sums of runs of Cg channels: groups[i] = sum of chan[i*Cg ..].  One group: the whole workgroup's work.  Ends with a barrier.
-__device__ inline void gn_group_sums(int W, int Cg, const float *chan, float *groups, float *red)
+// Sums of runs of `run` of the W channels: groups[i] = sum of chan[i*run ..].  Few long runs: each the whole workgroup's work.  Ends with
+// a barrier.
+__device__ inline void gn_group_sums(int W, int run, const float *chan, float *groups, float *red)
 {
-    if (W == Cg && Cg > 32) {
-        float s = 0.f;
-        for (int c = threadIdx.x; c < W; c += blockDim.x) s += chan[c];
-        s = wave_sum(s);
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (unsigned k = 1; k < blockDim.x / 64; ++k) s += red[k];
-            groups[0] = s;
+    if (run > 32) {
+        for (int g = 0; g < W / run; ++g) {
+            float s = 0.f;
+            for (int c = threadIdx.x; c < run; c += blockDim.x) s += chan[g * run + c];
+            s = wave_sum(s);
+            __syncthreads();  // red has been read
+            if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                for (unsigned k = 1; k < blockDim.x / 64; ++k) s += red[k];
+                groups[g] = s;
+            }
         }
     } else {
-        for (int g = threadIdx.x; g < W / Cg; g += blockDim.x) {
+        for (int g = threadIdx.x; g < W / run; g += blockDim.x) {
             float s = 0.f;
-            for (int i = 0; i < Cg; ++i) s += chan[g * Cg + i];
+            for (int i = 0; i < run; ++i) s += chan[g * run + i];
             groups[g] = s;
         }
     }
@@ -162,6 +177,8 @@ struct GnShape {
     int HW, C, G, Cg;
     int n0;  // first image of the launch
 };
+// S values of a vector that differ by group: one where vectors lie within groups (S == 1), else one to a channel.  Index of channel i's.
+template <int S> __device__ constexpr int gn_at(int i) { return S == 1 ? 0 : i; }
 
 // ---- a group in one workgroup ----------------------------------------------------------------------------------------------
 struct GnResident {
@@ -172,7 +189,7 @@ struct GnResident {
 // LDS: slots*W partial sums, W sums by channel, sums by group
 static size_t gn_lds_floats(const GnMap &m, int W, int planes) { return (size_t)planes * (m.slots * W + W) + 16 + planes * (size_t)W; }
 
-template <class T, int V, int E, int TH, int ACT, bool RES>
+template <class T, int V, int S, int E, int TH, int ACT, bool RES>
 __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, const T *__restrict__ x, const float *__restrict__ gamma,
                                                     const float *__restrict__ beta, float eps, const T *__restrict__ res, T *__restrict__ y,
                                                     float *__restrict__ save_mean, float *__restrict__ save_invstd)
@@ -183,7 +200,7 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);
     const int n = s.n0 + id / p.chunks, c0 = id % p.chunks * p.W;
     const GnThread t(p.map);
-    const int c = c0 + t.col * V, RL = p.map.row_lanes;
+    const int col = t.active ? t.col * V : 0, c = c0 + col, RL = p.map.row_lanes;
     const long base = (long)n * s.HW * s.C + c;
     typename Vec::Raw raw[E];
 #pragma unroll
@@ -203,13 +220,11 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
     gn_column_sums<V>(p.map, t, a, part, chan);
     gn_group_sums(p.W, s.Cg, chan, grp, red);
     const float m = (float)s.HW * (float)s.Cg;  // a division: the mean of equal values is that value, whatever their number
-    float mean[V];
-    const int col = t.active ? t.col * V : 0;
+    float mean[S];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        mean[i] = grp[(col + i) / s.Cg] / m;
-        a[i] = 0.f;
-    }
+    for (int i = 0; i < S; ++i) mean[i] = grp[(col + i) / s.Cg] / m;
+#pragma unroll
+    for (int i = 0; i < V; ++i) a[i] = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (t.active && t.row + e * RL < s.HW) {
@@ -217,26 +232,26 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
             Vec::unpack(raw[e], f);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float d = f[i] - mean[i];
+                const float d = f[i] - mean[gn_at<S>(i)];
                 a[i] = fmaf(d, d, a[i]);
             }
         }
     gn_column_sums<V>(p.map, t, a, part, chan);  // its first barrier: every thread has read grp
     gn_group_sums(p.W, s.Cg, chan, grp, red);
-    float scale[V], b[V];
-    if (t.active) {
-        gn_load_floats<V>(gamma + c, scale);
-        gn_load_floats<V>(beta + c, b);
+    if (!t.active) return;
+    float scale[V], b[V], invstd[S];
+    gn_load_floats<V>(gamma + c, scale);
+    gn_load_floats<V>(beta + c, b);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float invstd = 1.f / sqrtf(grp[(col + i) / s.Cg] / m + eps);
-            if (save_mean && t.row == 0 && (c + i) % s.Cg == 0) {
-                save_mean[(long)n * s.G + (c + i) / s.Cg] = mean[i];
-                save_invstd[(long)n * s.G + (c + i) / s.Cg] = invstd;
-            }
-            scale[i] *= invstd;
+    for (int i = 0; i < S; ++i) {
+        invstd[i] = 1.f / sqrtf(grp[(col + i) / s.Cg] / m + eps);
+        if (save_mean && t.row == 0 && (c + i) % s.Cg == 0) {
+            save_mean[(long)n * s.G + (c + i) / s.Cg] = mean[i];
+            save_invstd[(long)n * s.G + (c + i) / s.Cg] = invstd[i];
         }
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) scale[i] *= invstd[gn_at<S>(i)];
     constexpr int B = E < 4 ? E : 4;  // rows whose residuals are in flight together
 #pragma unroll
     for (int e0 = 0; e0 < E; e0 += B) {
@@ -244,16 +259,16 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
         if (RES)
 #pragma unroll
             for (int u = 0; u < B; ++u)
-                if (t.active && t.row + (e0 + u) * RL < s.HW) rr[u] = gn_load<T, V>(res + base + (long)(t.row + (e0 + u) * RL) * s.C);
+                if (t.row + (e0 + u) * RL < s.HW) rr[u] = gn_load<T, V>(res + base + (long)(t.row + (e0 + u) * RL) * s.C);
 #pragma unroll
         for (int u = 0; u < B; ++u)
-            if (t.active && t.row + (e0 + u) * RL < s.HW) {
+            if (t.row + (e0 + u) * RL < s.HW) {
                 float f[V], q[V];
                 Vec::unpack(raw[e0 + u], f);
                 if (RES) Vec::unpack(rr[u], q);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    float v = gn_pre(f[i], mean[i], scale[i], b[i]);
+                    float v = gn_pre(f[i], mean[gn_at<S>(i)], scale[i], b[i]);
                     if (RES) v += q[i];
                     f[i] = gn_act<ACT>(v);
                 }
@@ -262,25 +277,26 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
     }
 }
 
-// The operands of dz of one vector.
+// The operands of dz.
 template <class T> struct GnBwdIn {
     const T *x, *dy, *dy2, *res;
     const float *gamma, *beta, *mean, *invstd;
 };
 // A column's constants: mean, 1/sigma, scale and beta as the forward pass had them.
-template <int V> struct GnColumn {
-    float mean[V], inv[V], scale[V], beta[V], gamma[V];
+template <int V, int S> struct GnColumn {
+    float mean[S], inv[S], scale[V], beta[V];
     template <class T> __device__ GnColumn(const GnShape &s, const GnBwdIn<T> &in, int n, int c)
     {
-        gn_load_floats<V>(in.gamma + c, gamma);
+        gn_load_floats<V>(in.gamma + c, scale);
         gn_load_floats<V>(in.beta + c, beta);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
+        for (int i = 0; i < S; ++i) {
             const long at = (long)n * s.G + (c + i) / s.Cg;
             mean[i] = in.mean[at];
             inv[i] = in.invstd[at];
-            scale[i] = gamma[i] * inv[i];
         }
+#pragma unroll
+        for (int i = 0; i < V; ++i) scale[i] *= inv[gn_at<S>(i)];
     }
 };
 template <class T, int V, int ACT, bool RES, bool DY2> struct GnDz {
@@ -293,7 +309,7 @@ template <class T, int V, int ACT, bool RES, bool DY2> struct GnDz {
         if (RES) res = gn_load<T, V>(in.res + at);
     }
     // dz, and x - mean
-    __device__ void form(const GnColumn<V> &k, float *dz, float *d) const
+    template <int S> __device__ void form(const GnColumn<V, S> &k, float *dz, float *d) const
     {
         float f[V], g[V], q[V];
         GnVec<T, V>::unpack(x, f);
@@ -306,22 +322,25 @@ template <class T, int V, int ACT, bool RES, bool DY2> struct GnDz {
         if (RES) GnVec<T, V>::unpack(res, q);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            float u = gn_pre(f[i], k.mean[i], k.scale[i], k.beta[i]);
+            float u = gn_pre(f[i], k.mean[gn_at<S>(i)], k.scale[i], k.beta[i]);
             if (RES) u += q[i];
             dz[i] = gn_act_bwd<ACT>(g[i], u);
-            d[i] = f[i] - k.mean[i];
+            d[i] = f[i] - k.mean[gn_at<S>(i)];
         }
     }
 };
-// dx from dz, x - mean and the group's two means
-template <int V> __device__ inline void gn_dx(const GnColumn<V> &k, const float *dz, const float *d, const float *A, const float *B, float *out)
+// dx from dz, x - mean, and the group's means A of gamma*dz and B of gamma*dz*xhat, each times 1/sigma
+template <int V, int S> __device__ inline void gn_dx(const GnColumn<V, S> &k, const float *dz, const float *d, const float *A, const float *B, float *out)
 {
 #pragma unroll
-    for (int i = 0; i < V; ++i) out[i] = k.inv[i] * (fmaf(k.gamma[i], dz[i], -A[i]) - d[i] * k.inv[i] * B[i]);
+    for (int i = 0; i < V; ++i) {
+        const int g = gn_at<S>(i);
+        out[i] = fmaf(-d[i] * k.inv[g], B[g], fmaf(k.scale[i], dz[i], -A[g]));
+    }
 }
 
 // sums[0][n][c] = sum of dz over the image, sums[1][n][c] = sum of dz*xhat (NC = N*C apart)
-template <class T, int V, int E, int TH, int ACT, bool RES, bool DY2>
+template <class T, int V, int S, int E, int TH, int ACT, bool RES, bool DY2>
 __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, long NC, GnBwdIn<T> in, float *__restrict__ sums, T *__restrict__ dx,
                                                     T *__restrict__ dres)
 {
@@ -334,7 +353,7 @@ __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, lon
     const GnThread t(p.map);
     const int col = t.active ? t.col * V : 0, c = c0 + col, RL = p.map.row_lanes;
     const long base = (long)n * s.HW * s.C + c;
-    const GnColumn<V> k(s, in, n, c);
+    const GnColumn<V, S> k(s, in, n, c);
     typename Vec::Raw xr[E];
     float dz[E][V], a0[V], a1[V];
 #pragma unroll
@@ -355,7 +374,7 @@ __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, lon
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     a0[i] += dz[e0 + u][i];
-                    a1[i] = fmaf(dz[e0 + u][i], d[i] * k.inv[i], a1[i]);
+                    a1[i] = fmaf(dz[e0 + u][i], d[i] * k.inv[gn_at<S>(i)], a1[i]);
                 }
             }
     }
@@ -372,11 +391,11 @@ __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, lon
     gn_group_sums(p.W, s.Cg, chan0, grp0, red);
     gn_group_sums(p.W, s.Cg, chan1, grp1, red);
     const float m = (float)s.HW * (float)s.Cg;
-    float A[V], Bm[V];
+    float A[S], Bm[S];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        A[i] = grp0[(col + i) / s.Cg] / m;
-        Bm[i] = grp1[(col + i) / s.Cg] / m;
+    for (int i = 0; i < S; ++i) {
+        A[i] = grp0[(col + i) / s.Cg] / m * k.inv[i];
+        Bm[i] = grp1[(col + i) / s.Cg] / m * k.inv[i];
     }
 #pragma unroll
     for (int e = 0; e < E; ++e)
@@ -384,50 +403,80 @@ __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, lon
             float f[V];
             Vec::unpack(xr[e], f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) f[i] -= k.mean[i];
+            for (int i = 0; i < V; ++i) f[i] -= k.mean[gn_at<S>(i)];
             const long at = base + (long)(t.row + e * RL) * s.C;
             if (dres) gn_store<T, V>(dres + at, dz[e]);
-            gn_dx<V>(k, dz[e], f, A, Bm, f);
+            gn_dx<V, S>(k, dz[e], f, A, Bm, f);
             gn_store<T, V>(dx + at, f);
         }
 }
 
 // ---- two passes over memory ------------------------------------------------------------------------------------------------
-// A workgroup takes a band of rows of a run of columns, whatever groups they are in; partial results by channel lie at [image][band][C],
-// a second plane behind the first.
-constexpr int kGnThreads = 512, kGnRows = 8;  // rows of a thread in a band
+// A workgroup takes a band of rows of a run of channels: whole groups, or a piece of one where a group has more vectors than
+// that.  Partial results lie at [image][group][piece][band], a second plane behind the first.
+constexpr int kGnThreads = 512, kGnCols = 256;  // vectors of a row in a workgroup, at most: LDS stays below 48 KB
+constexpr int kGnStatRows = 8, kGnSumRows = 16;  // rows of a thread in a band
 struct GnBands {
     GnMap map;
-    int W, chunks;   // channels of a workgroup (the last run of an image may be short), runs of an image
-    int rows, bands; // rows of a band (the last may be short), bands of an image
-    long plane;      // floats of a plane of partial results
+    int W, chunks;    // channels of a workgroup (fewer in the last of an image, or of a group in pieces), workgroups to a row
+    int pieces;       // pieces of a group
+    int rows, bands;  // rows of a band (the last may be short), bands of an image
+    long plane;       // floats of a plane of partial results
 };
-__device__ inline int gn_band_rows(const GnShape &s, const GnBands &p, int band) { return min(p.rows, s.HW - band * p.rows); }
+struct GnPlace {
+    int image, band, rows, c0, width;  // the workgroup's
+    int run, first;                    // channels of a group in it, index of its first partial result's group and piece
+    // xcd_contiguous, so that an XCD's workgroups are neighbours; `back`: each XCD's in falling order, so that what the pass before read
+    // last is read first, while the caches hold it
+    __device__ GnPlace(const GnShape &s, const GnBands &p, int block, int blocks, bool back)
+    {
+        const int n8 = blocks & ~7;
+        int id = block;
+        if (block < n8) id = (block & 7) * (n8 >> 3) + (back ? (n8 >> 3) - 1 - (block >> 3) : block >> 3);
+        const int chunk = id % p.chunks;
+        id /= p.chunks;
+        band = id % p.bands;
+        image = id / p.bands;
+        rows = min(p.rows, s.HW - band * p.rows);
+        if (p.pieces == 1) {
+            c0 = chunk * p.W;
+            width = min(p.W, s.C - c0);
+            run = s.Cg;
+            first = c0 / s.Cg;
+        } else {
+            const int g = chunk / p.pieces, piece = chunk % p.pieces;
+            c0 = g * s.Cg + piece * p.W;
+            width = run = min(p.W, s.Cg - piece * p.W);
+            first = chunk;
+        }
+    }
+    __device__ float *partial(const GnShape &s, const GnBands &p, float *parts, int i) const
+    {
+        return parts + ((long)image * s.G * p.pieces + first + i) * p.bands + band;
+    }
+};
 
-// mean and sum of squared deviations of every channel over a band
-template <class T, int V>
-__global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnShape s, GnBands p, const T *__restrict__ x, float *__restrict__ part_out)
+// mean and sum of squared deviations of every group over a band
+template <class T, int V, int S>
+__global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnShape s, GnBands p, const T *__restrict__ x, float *__restrict__ parts)
 {
     typedef GnVec<T, V> Vec;
     extern __shared__ float lds[];
-    float *part = lds, *chan = part + p.map.slots * p.W;
-    int id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int chunk = id % p.chunks;
-    id /= p.chunks;
-    const int band = id % p.bands, image = id / p.bands;
+    float *part = lds, *chan = part + p.map.slots * p.W, *red = chan + p.W, *grp = red + 16;
+    const GnPlace pl(s, p, blockIdx.x, gridDim.x, false);
     GnThread t(p.map);
-    const int c = chunk * p.W + t.col * V, r0 = band * p.rows, rows = gn_band_rows(s, p, band), RL = p.map.row_lanes;
-    t.active = t.active && c < s.C;
-    const T *from = x + ((long)(s.n0 + image) * s.HW + r0) * s.C + c;
-    typename Vec::Raw raw[kGnRows];
+    t.active = t.active && t.col * V < pl.width;
+    const int col = t.active ? t.col * V : 0, rows = pl.rows, RL = p.map.row_lanes;
+    const T *from = x + ((long)(s.n0 + pl.image) * s.HW + (long)pl.band * p.rows) * s.C + pl.c0 + col;
+    typename Vec::Raw raw[kGnStatRows];
 #pragma unroll
-    for (int e = 0; e < kGnRows; ++e)
+    for (int e = 0; e < kGnStatRows; ++e)
         if (e * RL < rows && t.active) raw[e] = gn_load<T, V>(from + (long)min(t.row + e * RL, rows - 1) * s.C);
-    float a[V], mean[V];
+    float a[V], mean[S];
 #pragma unroll
     for (int i = 0; i < V; ++i) a[i] = 0.f;
 #pragma unroll
-    for (int e = 0; e < kGnRows; ++e)
+    for (int e = 0; e < kGnStatRows; ++e)
         if (t.active && t.row + e * RL < rows) {
             float f[V];
             Vec::unpack(raw[e], f);
@@ -435,32 +484,28 @@ __global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnShape s, GnBands
             for (int i = 0; i < V; ++i) a[i] += f[i];
         }
     gn_column_sums<V>(p.map, t, a, part, chan);
-    const int col = t.active ? t.col * V : 0;
+    gn_group_sums(pl.width, pl.run, chan, grp, red);
+    const float m = (float)rows * (float)pl.run;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        mean[i] = chan[col + i] / (float)rows;
-        a[i] = 0.f;
-    }
+    for (int i = 0; i < S; ++i) mean[i] = grp[(col + i) / pl.run] / m;
 #pragma unroll
-    for (int e = 0; e < kGnRows; ++e)
+    for (int i = 0; i < V; ++i) a[i] = 0.f;
+#pragma unroll
+    for (int e = 0; e < kGnStatRows; ++e)
         if (t.active && t.row + e * RL < rows) {
             float f[V];
             Vec::unpack(raw[e], f);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float d = f[i] - mean[i];
+                const float d = f[i] - mean[gn_at<S>(i)];
                 a[i] = fmaf(d, d, a[i]);
             }
         }
-    gn_column_sums<V>(p.map, t, a, part, chan);  // its first barrier: every thread has its mean
-    float *out = part_out + ((long)image * p.bands + band) * s.C + c;
-    if (t.active && t.row == 0) {
-#pragma unroll
-        for (int i = 0; i < V; i += 4) {
-            *reinterpret_cast<float4 *>(out + i) = make_float4(mean[i], mean[i + 1], mean[i + 2], mean[i + 3]);
-            *reinterpret_cast<float4 *>(out + p.plane + i) = make_float4(chan[col + i], chan[col + i + 1], chan[col + i + 2], chan[col + i + 3]);
-        }
-    }
+    const int count = pl.width / pl.run;
+    for (int k = threadIdx.x; k < count; k += kGnThreads) *pl.partial(s, p, parts, k) = grp[k] / m;
+    gn_column_sums<V>(p.map, t, a, part, chan);  // its first barrier: every thread has read grp
+    gn_group_sums(pl.width, pl.run, chan, grp, red);
+    for (int k = threadIdx.x; k < count; k += kGnThreads) *pl.partial(s, p, parts + p.plane, k) = grp[k];
 }
 
 constexpr int kGnMergeThreads = 256;
@@ -477,58 +522,55 @@ __device__ inline double gn_block_sum(double v, double *red)
     return v;
 }
 
-// A group's statistics from its channels' in all bands; in 64 bits, since there may be thousands.
-__global__ __launch_bounds__(kGnMergeThreads) void gn_stats_merge_kernel(GnShape s, GnBands p, const float *__restrict__ part, float eps,
+// A group's statistics from those of its bands; in 64 bits, since there may be thousands.
+__global__ __launch_bounds__(kGnMergeThreads) void gn_stats_merge_kernel(GnShape s, GnBands p, const float *__restrict__ parts, float eps,
                                                                          float *__restrict__ mean_out, float *__restrict__ invstd_out)
 {
     __shared__ double red[kGnMergeThreads / 64];
-    const int image = blockIdx.x / s.G, g = blockIdx.x % s.G;
-    const float *from = part + (long)image * p.bands * s.C + g * s.Cg;
-    const int count = p.bands * s.Cg;
+    const int count = p.bands * p.pieces;
+    const float *from = parts + (long)blockIdx.x * count;
+    auto values = [&](int i) {  // how many partial result i stands for
+        const int piece = i / p.bands;
+        return (float)min(p.rows, s.HW - (i - piece * p.bands) * p.rows) * (float)(p.pieces == 1 ? s.Cg : min(p.W, s.Cg - piece * p.W));
+    };
     double a = 0.;
-    for (int i = threadIdx.x; i < count; i += kGnMergeThreads) {
-        const int b = i / s.Cg;
-        a += (double)gn_band_rows(s, p, b) * from[(long)b * s.C + i - b * s.Cg];
-    }
+    for (int i = threadIdx.x; i < count; i += kGnMergeThreads) a += (double)values(i) * from[i];
     const double m = (double)s.HW * s.Cg, mean = gn_block_sum(a, red) / m;
     a = 0.;
     for (int i = threadIdx.x; i < count; i += kGnMergeThreads) {
-        const int b = i / s.Cg;
-        const long at = (long)b * s.C + i - b * s.Cg;
-        const double d = from[at] - mean;
-        a += from[p.plane + at] + gn_band_rows(s, p, b) * d * d;
+        const double d = from[i] - mean;
+        a += from[p.plane + i] + values(i) * d * d;
     }
     const float var = (float)(gn_block_sum(a, red) / m);
     if (threadIdx.x == 0) {
-        const long at = (long)(s.n0 + image) * s.G + g;
+        const long at = (long)s.n0 * s.G + blockIdx.x;
         mean_out[at] = (float)mean;
         invstd_out[at] = 1.f / sqrtf(var + eps);
     }
 }
 
-template <class T, int V, int ACT, bool RES>
+template <class T, int V, int S, int ACT, bool RES>
 __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnShape s, GnBands p, const T *__restrict__ x, const float *__restrict__ gamma,
                                                               const float *__restrict__ beta, const float *__restrict__ mean_in,
                                                               const float *__restrict__ invstd, const T *__restrict__ res, T *__restrict__ y)
 {
     typedef GnVec<T, V> Vec;
-    int id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int chunk = id % p.chunks;
-    id /= p.chunks;
-    const int band = id % p.bands, n = s.n0 + id / p.bands;
+    const GnPlace pl(s, p, blockIdx.x, gridDim.x, true);
     const GnThread t(p.map);
-    const int c = chunk * p.W + t.col * V, rows = gn_band_rows(s, p, band), RL = p.map.row_lanes;
-    if (!t.active || c >= s.C) return;
-    const long base = ((long)n * s.HW + (long)band * p.rows) * s.C + c;
-    float mean[V], scale[V], b[V];
+    const int c = pl.c0 + t.col * V, rows = pl.rows, RL = p.map.row_lanes, n = s.n0 + pl.image;
+    if (!t.active || t.col * V >= pl.width) return;
+    const long base = ((long)n * s.HW + (long)pl.band * p.rows) * s.C + c;
+    float mean[S], scale[V], b[V], inv[S];
     gn_load_floats<V>(gamma + c, scale);
     gn_load_floats<V>(beta + c, b);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
+    for (int i = 0; i < S; ++i) {
         const long at = (long)n * s.G + (c + i) / s.Cg;
         mean[i] = mean_in[at];
-        scale[i] *= invstd[at];
+        inv[i] = invstd[at];
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) scale[i] *= inv[gn_at<S>(i)];
     constexpr int B = 4;
     for (int r0 = t.row; r0 < rows; r0 += B * RL) {
         typename Vec::Raw xr[B], rr[B];
@@ -546,7 +588,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnShape s, GnBands
                 if (RES) Vec::unpack(rr[u], q);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    float v = gn_pre(f[i], mean[i], scale[i], b[i]);
+                    float v = gn_pre(f[i], mean[gn_at<S>(i)], scale[i], b[i]);
                     if (RES) v += q[i];
                     f[i] = gn_act<ACT>(v);
                 }
@@ -555,21 +597,19 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnShape s, GnBands
     }
 }
 
-// sums of dz and dz*xhat of every channel over a band
-template <class T, int V, int ACT, bool RES, bool DY2>
-__global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape s, GnBands p, GnBwdIn<T> in, float *__restrict__ part_out)
+// Sums over a band: by channel of dz and dz*xhat (chans, [image][band][C], a second plane `chan_plane` behind), by group of both times gamma.
+template <class T, int V, int S, int ACT, bool RES, bool DY2>
+__global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape s, GnBands p, GnBwdIn<T> in, float *__restrict__ chans, long chan_plane,
+                                                             float *__restrict__ parts)
 {
     extern __shared__ float lds[];
-    float *part = lds, *chan0 = part + p.map.slots * p.W, *chan1 = chan0 + p.W;
-    int id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int chunk = id % p.chunks;
-    id /= p.chunks;
-    const int band = id % p.bands, image = id / p.bands, n = s.n0 + image;
+    float *part = lds, *chan0 = part + p.map.slots * p.W, *chan1 = chan0 + p.W, *red = chan1 + p.W, *grp = red + 16;
+    const GnPlace pl(s, p, blockIdx.x, gridDim.x, false);
     GnThread t(p.map);
-    t.active = t.active && chunk * p.W + t.col * V < s.C;
-    const int col = t.active ? t.col * V : 0, c = chunk * p.W + col, rows = gn_band_rows(s, p, band), RL = p.map.row_lanes;
-    const long base = ((long)n * s.HW + (long)band * p.rows) * s.C + c;
-    const GnColumn<V> k(s, in, n, c);
+    t.active = t.active && t.col * V < pl.width;
+    const int col = t.active ? t.col * V : 0, c = pl.c0 + col, rows = pl.rows, RL = p.map.row_lanes, n = s.n0 + pl.image;
+    const long base = ((long)n * s.HW + (long)pl.band * p.rows) * s.C + c;
+    const GnColumn<V, S> k(s, in, n, c);
     float a0[V], a1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) a0[i] = a1[i] = 0.f;
@@ -588,83 +628,107 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape s, GnBands 
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         a0[i] += dz[i];
-                        a1[i] = fmaf(dz[i], d[i] * k.inv[i], a1[i]);
+                        a1[i] = fmaf(dz[i], d[i] * k.inv[gn_at<S>(i)], a1[i]);
                     }
                 }
         }
     gn_column_sums<V>(p.map, t, a0, part, chan0);
     gn_column_sums<V>(p.map, t, a1, part, chan1);
-    float *out = part_out + ((long)image * p.bands + band) * s.C + c;
-    if (t.active && t.row == 0) {
-#pragma unroll
-        for (int i = 0; i < V; i += 4) {
-            *reinterpret_cast<float4 *>(out + i) = make_float4(chan0[col + i], chan0[col + i + 1], chan0[col + i + 2], chan0[col + i + 3]);
-            *reinterpret_cast<float4 *>(out + p.plane + i) = make_float4(chan1[col + i], chan1[col + i + 1], chan1[col + i + 2], chan1[col + i + 3]);
-        }
+    float *out = chans + ((long)n * p.bands + pl.band) * s.C + pl.c0;
+    for (int i = threadIdx.x; i < pl.width; i += kGnThreads) {
+        const float g = in.gamma[pl.c0 + i];
+        out[i] = chan0[i];
+        out[chan_plane + i] = chan1[i];
+        chan0[i] *= g;
+        chan1[i] *= g;
     }
+    __syncthreads();
+    const int count = pl.width / pl.run;
+    gn_group_sums(pl.width, pl.run, chan0, grp, red);
+    for (int i = threadIdx.x; i < count; i += kGnThreads) *pl.partial(s, p, parts, i) = grp[i];
+    gn_group_sums(pl.width, pl.run, chan1, grp + count, red);
+    for (int i = threadIdx.x; i < count; i += kGnThreads) *pl.partial(s, p, parts + p.plane, i) = grp[count + i];
 }
 
-// The bands' sums, by image and channel, and the group's two means of gamma*dz and gamma*dz*xhat
-__global__ __launch_bounds__(kGnMergeThreads) void gn_sums_merge_kernel(GnShape s, GnBands p, const float *__restrict__ part,
-                                                                        const float *__restrict__ gamma, long NC, float *__restrict__ sums,
-                                                                        float *__restrict__ means)
+// The group's means of gamma*dz and gamma*dz*xhat, from its bands' sums.
+__global__ __launch_bounds__(kGnMergeThreads) void gn_sums_merge_kernel(GnShape s, GnBands p, const float *__restrict__ parts, float *__restrict__ means)
 {
-    __shared__ double red[kGnMergeThreads / 64], acc[2][kGnMergeThreads];
-    const int image = blockIdx.x / s.G, g = blockIdx.x % s.G, n = s.n0 + image;
-    const float *from = part + (long)image * p.bands * s.C + g * s.Cg;
-    const int wide = min(s.Cg, kGnMergeThreads), slices = kGnMergeThreads / wide, ci = threadIdx.x % wide, sl = threadIdx.x / wide;
+    __shared__ double red[kGnMergeThreads / 64];
+    const int count = p.bands * p.pieces;
+    const float *from = parts + (long)blockIdx.x * count;
     double A = 0., B = 0.;
-    for (int c0 = 0; c0 < s.Cg; c0 += wide) {
-        double a0 = 0., a1 = 0.;
-        if (sl < slices && c0 + ci < s.Cg)
-            for (int b = sl; b < p.bands; b += slices) {
-                a0 += from[(long)b * s.C + c0 + ci];
-                a1 += from[p.plane + (long)b * s.C + c0 + ci];
-            }
-        __syncthreads();
-        acc[0][threadIdx.x] = a0;
-        acc[1][threadIdx.x] = a1;
-        __syncthreads();
-        if (sl == 0 && c0 + ci < s.Cg) {
-            for (int k = 1; k < slices; ++k) {
-                a0 += acc[0][k * wide + ci];
-                a1 += acc[1][k * wide + ci];
-            }
-            const int c = g * s.Cg + c0 + ci;
-            sums[(long)n * s.C + c] = (float)a0;
-            sums[NC + (long)n * s.C + c] = (float)a1;
-            A += gamma[c] * a0;
-            B += gamma[c] * a1;
-        }
+    for (int i = threadIdx.x; i < count; i += kGnMergeThreads) {
+        A += from[i];
+        B += from[p.plane + i];
     }
     const double m = (double)s.HW * s.Cg;
     A = gn_block_sum(A, red) / m;
     B = gn_block_sum(B, red) / m;
     if (threadIdx.x == 0) {
-        means[2 * ((long)image * s.G + g)] = (float)A;
-        means[2 * ((long)image * s.G + g) + 1] = (float)B;
+        means[2 * (long)blockIdx.x] = (float)A;
+        means[2 * (long)blockIdx.x + 1] = (float)B;
     }
 }
 
-template <class T, int V, int ACT, bool RES, bool DY2>
-__global__ __launch_bounds__(kGnThreads) void gn_bwd_apply_kernel(GnShape s, GnBands p, GnBwdIn<T> in, const float *__restrict__ means,
-                                                                  T *__restrict__ dx, T *__restrict__ dres)
+// dgamma and dbeta: sums over `rows` rows of C channels, a workgroup's 16 channels.  Thread = (row lane, channel); each adds every 32nd row,
+// four at a time; the row lanes are added in pairs, pairs of pairs, ...
+constexpr int kGnParamCh = 16, kGnParamRows = kGnThreads / kGnParamCh;
+__device__ inline void gn_params(int block, long rows, int C, const float *__restrict__ chans, float *__restrict__ dgamma, float *__restrict__ dbeta,
+                                 float (*red)[kGnThreads])
 {
-    int id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int chunk = id % p.chunks;
-    id /= p.chunks;
-    const int band = id % p.bands, image = id / p.bands, n = s.n0 + image;
-    const GnThread t(p.map);
-    const int c = chunk * p.W + t.col * V, rows = gn_band_rows(s, p, band), RL = p.map.row_lanes;
-    if (!t.active || c >= s.C) return;
-    const long base = ((long)n * s.HW + (long)band * p.rows) * s.C + c;
-    const GnColumn<V> k(s, in, n, c);
-    float A[V], Bm[V];
+    const int cl = threadIdx.x % kGnParamCh, rl = threadIdx.x / kGnParamCh, c = block * kGnParamCh + cl;
+    float b[4] = {0.f, 0.f, 0.f, 0.f}, g[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c < C)
+        for (long r0 = rl; r0 < rows; r0 += 4 * kGnParamRows)
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const long at = 2 * ((long)image * s.G + (c + i) / s.Cg);
-        A[i] = means[at];
-        Bm[i] = means[at + 1];
+            for (int u = 0; u < 4; ++u)
+                if (r0 + u * kGnParamRows < rows) {
+                    b[u] += chans[(r0 + u * kGnParamRows) * C + c];
+                    g[u] += chans[(rows + r0 + u * kGnParamRows) * C + c];
+                }
+    red[0][threadIdx.x] = (b[0] + b[1]) + (b[2] + b[3]);
+    red[1][threadIdx.x] = (g[0] + g[1]) + (g[2] + g[3]);
+#pragma unroll
+    for (int half = kGnParamRows / 2; half; half /= 2) {
+        __syncthreads();
+        if (rl < half) {
+            red[0][threadIdx.x] += red[0][threadIdx.x + half * kGnParamCh];
+            red[1][threadIdx.x] += red[1][threadIdx.x + half * kGnParamCh];
+        }
+    }
+    if (rl == 0 && c < C) {
+        dbeta[c] = red[0][threadIdx.x];
+        dgamma[c] = red[1][threadIdx.x];
+    }
+}
+__global__ __launch_bounds__(kGnThreads) void gn_params_kernel(long rows, int C, const float *__restrict__ chans, float *__restrict__ dgamma,
+                                                               float *__restrict__ dbeta)
+{
+    __shared__ float red[2][kGnThreads];
+    gn_params(blockIdx.x, rows, C, chans, dgamma, dbeta, red);
+}
+
+// The first param_blocks workgroups add up dgamma and dbeta (they need nothing of the others).
+template <class T, int V, int S, int ACT, bool RES, bool DY2>
+__global__ __launch_bounds__(kGnThreads) void gn_bwd_apply_kernel(GnShape s, GnBands p, GnBwdIn<T> in, const float *__restrict__ means,
+                                                                  T *__restrict__ dx, T *__restrict__ dres, int param_blocks, long param_rows,
+                                                                  const float *__restrict__ chans, float *__restrict__ dgamma,
+                                                                  float *__restrict__ dbeta)
+{
+    __shared__ float red[2][kGnThreads];
+    if ((int)blockIdx.x < param_blocks) return gn_params(blockIdx.x, param_rows, s.C, chans, dgamma, dbeta, red);
+    const GnPlace pl(s, p, blockIdx.x - param_blocks, gridDim.x - param_blocks, true);
+    const GnThread t(p.map);
+    const int c = pl.c0 + t.col * V, rows = pl.rows, RL = p.map.row_lanes, n = s.n0 + pl.image;
+    if (!t.active || t.col * V >= pl.width) return;
+    const long base = ((long)n * s.HW + (long)pl.band * p.rows) * s.C + c;
+    const GnColumn<V, S> k(s, in, n, c);
+    float A[S], Bm[S];
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        const long at = 2 * ((long)pl.image * s.G + (c + i) / s.Cg);
+        A[i] = means[at] * k.inv[i];
+        Bm[i] = means[at + 1] * k.inv[i];
     }
     constexpr int B = 4;
     for (int r0 = t.row; r0 < rows; r0 += B * RL) {
@@ -679,81 +743,70 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_apply_kernel(GnShape s, GnB
                 q[u].form(k, dz, d);
                 const long at = base + (long)(r0 + u * RL) * s.C;
                 if (dres) gn_store<T, V>(dres + at, dz);
-                gn_dx<V>(k, dz, d, A, Bm, d);
+                gn_dx<V, S>(k, dz, d, A, Bm, d);
                 gn_store<T, V>(dx + at, d);
             }
     }
 }
 
-// dgamma and dbeta: the images' sums; a workgroup takes 64 channels, a wavefront every 16th image
-constexpr int kGnParamWaves = 16;
-__global__ __launch_bounds__(64 * kGnParamWaves) void gn_params_kernel(int N, int C, const float *__restrict__ sums, float *__restrict__ dgamma,
-                                                                       float *__restrict__ dbeta)
-{
-    __shared__ float part[2][kGnParamWaves][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = min(blockIdx.x * 64 + lane, (unsigned)C - 1);
-    const long NC = (long)N * C;
-    float b[4] = {0.f, 0.f, 0.f, 0.f}, g[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int n0 = wave; n0 < N; n0 += 4 * kGnParamWaves)
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (n0 + u * kGnParamWaves < N) {
-                b[u] += sums[(long)(n0 + u * kGnParamWaves) * C + c];
-                g[u] += sums[NC + (long)(n0 + u * kGnParamWaves) * C + c];
-            }
-    part[0][wave][lane] = (b[0] + b[1]) + (b[2] + b[3]);
-    part[1][wave][lane] = (g[0] + g[1]) + (g[2] + g[3]);
-    __syncthreads();
-    if (threadIdx.x < 128) {
-        float v[kGnParamWaves];
-#pragma unroll
-        for (int w = 0; w < kGnParamWaves; ++w) v[w] = part[wave][w][lane];
-#pragma unroll
-        for (int half = kGnParamWaves / 2; half; half /= 2)
-#pragma unroll
-            for (int w = 0; w < half; ++w) v[w] += v[w + half];
-        if (blockIdx.x * 64 + lane < (unsigned)C) (wave == 0 ? dbeta : dgamma)[c] = v[0];
-    }
-}
-
 // ---- host side -------------------------------------------------------------------------------------------------------------
 static int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
+// Channels that are whole groups and whole vectors of V.
+static int gn_unit(int Cg, int V) { return Cg / gcd(Cg, V) * V; }
 
-// Channels of a workgroup: whole groups and whole vectors, of at least `bytes` of a row where the image has them.  0: groups and
-// vectors of V do not meet below C.
+// Channels of a workgroup that keeps its groups: whole units, of at least `bytes` of a row where the image has them.
 static int gn_run(int C, int Cg, int V, int size, int bytes)
 {
-    if (C % V) return 0;
-    const int unit = Cg / gcd(Cg, V) * V;
-    if (C % unit) return 0;
-    for (int j = 1; j <= C / unit; ++j)
-        if (C / unit % j == 0 && (j * unit * size >= bytes || j == C / unit)) return j * unit;
+    const int unit = gn_unit(Cg, V);
+    for (int j = 1; j < C / unit; ++j)
+        if (C / unit % j == 0 && j * unit * size >= bytes) return j * unit;
     return C;
 }
 
 constexpr int kGnSegment = 64;
 // The two-pass kernels' cut.
-template <class T> static GnBands gn_bands(int n, int HW, int C, int V)
+static GnBands gn_bands(int n, int HW, int C, int Cg, int V, int thread_rows)
 {
     GnBands p;
-    const int cols = C / V;
-    p.chunks = ceil_div(cols, kGnThreads);
-    p.W = ceil_div(cols, p.chunks) * V;
+    const int unit = gn_unit(Cg, V), units = C / unit, most = kGnCols * V / unit;  // units of a workgroup
+    if (most) {
+        p.chunks = ceil_div(units, most);
+        p.W = ceil_div(units, p.chunks) * unit;
+        p.pieces = 1;
+    } else {  // V divides Cg (see gn_vector)
+        p.pieces = ceil_div(Cg / V, kGnCols);
+        p.W = ceil_div(Cg / V, p.pieces) * V;
+        p.chunks = C / Cg * p.pieces;
+    }
     p.map = GnMap::of(p.W / V, kGnThreads);
-    p.rows = p.map.row_lanes * kGnRows;
+    p.rows = p.map.row_lanes * thread_rows;
     p.bands = ceil_div(HW, p.rows);
-    p.plane = (long)n * p.bands * C;
+    p.plane = (long)n * (C / Cg) * p.pieces * p.bands;
     return p;
 }
 
-// Workspace: sums by image and channel (two planes), statistics or means by image and group (two values), partial results (two planes).
-struct GnRoom { size_t sums, pairs, parts; size_t floats() const { return sums + pairs + parts; } };
+// Vector width: the widest that lies within groups; four channels also across groups, unless whole groups of whole vectors are then more
+// than a workgroup takes.
+static int gn_vector(int Cg, int size)
+{
+    if (size == 2 && Cg % 8 == 0) return 8;
+    return Cg % 4 == 0 || gn_unit(Cg, 4) <= 4 * kGnCols ? 4 : 1;
+}
+
+// Workspace: statistics or means by image and group (two values), then partial results by group and by channel (two planes each); a
+// workgroup that keeps its groups leaves sums by image and channel.  Enough for either element type.
+struct GnRoom { size_t pairs, parts, chans; size_t floats() const { return pairs + parts + chans; } };
 static GnRoom gn_room(int n, int c, int HW, int groups)
 {
-    const GnBands p = gn_bands<float>(n, HW, c, 4);  // vectors of four channels: the most bands
-    const GnBands q = c % 8 == 0 ? gn_bands<float>(n, HW, c, 8) : p;
-    const long plane = p.plane > q.plane ? p.plane : q.plane;
-    return {((size_t)2 * n * c + 3) & ~(size_t)3, ((size_t)2 * n * groups + 3) & ~(size_t)3, (size_t)2 * plane};
+    GnRoom r{((size_t)2 * n * groups + 3) & ~(size_t)3, 0, (size_t)2 * n * c};
+    for (int size : {2, 4})
+        for (int rows : {kGnStatRows, kGnSumRows}) {
+            const GnBands p = gn_bands(n, HW, c, c / groups, gn_vector(c / groups, size), rows);
+            const size_t parts = ((size_t)2 * p.plane + 3) & ~(size_t)3, chans = (size_t)2 * n * p.bands * c;
+            if (parts > r.parts) r.parts = parts;
+            if (rows == kGnSumRows && chans > r.chans) r.chans = chans;
+        }
+    return r;
 }
 
 static int gn_check(const char *who, int n, int c, int h, int w, int layout, int groups, int act)
@@ -779,13 +832,16 @@ template <class F> static void gn_with(bool b, F f)
     if (b) f(std::true_type{});
     else f(std::false_type{});
 }
-// f(V) with the widest vectors that runs of whole groups are made of
-template <class T, class F> static void gn_with_vector(int c, int Cg, F f)
+// f(V, S): vector width, and how many groups' values a vector may need
+template <class T, class F> static void gn_with_vector(int Cg, F f)
 {
+    const int V = gn_vector(Cg, sizeof(T));
     if constexpr (std::is_same<T, bf16_t>::value) {
-        if (c % 8 == 0) return f(std::integral_constant<int, 8>{});
+        if (V == 8) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
     }
-    f(std::integral_constant<int, 4>{});
+    if (V == 1) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
+    if (Cg % 4 == 0) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+    f(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
 }
 
 // Images of one launch: below 2^31 threads of it.
@@ -796,14 +852,15 @@ static int gn_images(int n, long workgroups_each, int threads)
 }
 
 template <int TH, int E> struct GnSize { static constexpr int threads = TH, rows = E; };
-// Tries sizes in turn: f(size) for the first whose threads hold all rows.
-template <class S, class... More, class F> static bool gn_first_fit_of(int HW, int cols, F f)
+// Tries sizes in turn: f(size) for the first whose threads hold all rows (of W channels, in vectors of V; `planes` sums of each).
+template <class S, class... More, class F> static bool gn_first_fit_of(int HW, int W, int V, int planes, F f)
 {
-    if (cols <= S::threads && (long)GnMap::of(cols, S::threads).row_lanes * S::rows >= HW) {
+    const GnMap m = GnMap::of(W / V, S::threads);
+    if (W / V <= S::threads && (long)m.row_lanes * S::rows >= HW && gn_lds_floats(m, W, planes) <= 16384) {
         f(S{});
         return true;
     }
-    if constexpr (sizeof...(More) > 0) return gn_first_fit_of<More...>(HW, cols, f);
+    if constexpr (sizeof...(More) > 0) return gn_first_fit_of<More...>(HW, W, V, planes, f);
     return false;
 }
 
@@ -823,43 +880,43 @@ static int gn_fwd_impl(const char *who, int n, int c, int h, int w, int layout, 
     const GnRoom room = gn_room(n, c, HW, groups);
     RN50_REQUIRE(ws_bytes >= room.floats() * sizeof(float), RN50_EWORKSPACE, "%s: workspace too small", who);
     hipStream_t st = (hipStream_t)stream;
-    gn_with_vector<T>(c, Cg, [&](auto vec) {
-        constexpr int V = decltype(vec)::value;
-        const int W = gn_run(c, Cg, V, sizeof(T), kGnSegment);
-        bool done = false;
-        if (W)
-            done = gn_first_fit_of<GnSize<256, 4>, GnSize<256, 8>, GnSize<512, 8>, GnSize<512, 16>, GnSize<1024, 16>>(HW, W / V, [&](auto size) {
-                constexpr int TH = decltype(size)::threads, E = decltype(size)::rows;
-                const GnResident p{GnMap::of(W / V, TH), W, c / W};
-                const size_t lds = gn_lds_floats(p.map, W, 1) * sizeof(float);
-                const int each = gn_images(n, p.chunks, TH);
-                for (int n0 = 0; n0 < n; n0 += each) {
-                    const GnShape s{HW, c, groups, Cg, n0};
-                    const dim3 grid((unsigned)((n - n0 < each ? n - n0 : each) * p.chunks));
-                    gn_with_act(act, [&](auto a) {
-                        gn_with(res != nullptr, [&](auto r) {
-                            hipLaunchKernelGGL((gn_fwd_kernel<T, V, E, TH, decltype(a)::value, decltype(r)::value>), grid, dim3(TH), lds, st, s, p, x,
-                                               gamma, beta, eps, res, y, save_mean, save_invstd);
+    gn_with_vector<T>(Cg, [&](auto vec, auto per_group) {
+        constexpr int V = decltype(vec)::value, S = decltype(per_group)::value;
+        if constexpr (V > 1) {
+            const int W = gn_run(c, Cg, V, sizeof(T), kGnSegment);
+            if (gn_first_fit_of<GnSize<256, 4>, GnSize<256, 8>, GnSize<512, 8>, GnSize<512, 16>, GnSize<1024, 16>>(HW, W, V, 1, [&](auto size) {
+                    constexpr int TH = decltype(size)::threads, E = decltype(size)::rows;
+                    const GnResident p{GnMap::of(W / V, TH), W, c / W};
+                    const size_t lds = gn_lds_floats(p.map, W, 1) * sizeof(float);
+                    const int each = gn_images(n, p.chunks, TH);
+                    for (int n0 = 0; n0 < n; n0 += each) {
+                        const GnShape s{HW, c, groups, Cg, n0};
+                        const dim3 grid((unsigned)((n - n0 < each ? n - n0 : each) * p.chunks));
+                        gn_with_act(act, [&](auto a) {
+                            gn_with(res != nullptr, [&](auto r) {
+                                hipLaunchKernelGGL((gn_fwd_kernel<T, V, S, E, TH, decltype(a)::value, decltype(r)::value>), grid, dim3(TH), lds, st,
+                                                   s, p, x, gamma, beta, eps, res, y, save_mean, save_invstd);
+                            });
                         });
-                    });
-                }
-            });
-        if (done) return;
-        const GnBands p = gn_bands<T>(n, HW, c, V);
-        float *mean = save_mean ? save_mean : (float *)ws + room.sums, *invstd = save_invstd ? save_invstd : mean + (size_t)n * groups;
-        float *part = (float *)ws + room.sums + room.pairs;
-        const size_t lds = (size_t)(p.map.slots + 1) * p.W * sizeof(float);
+                    }
+                }))
+                return;
+        }
+        const GnBands p = gn_bands(n, HW, c, Cg, V, kGnStatRows);
+        float *mean = save_mean ? save_mean : (float *)ws, *invstd = save_invstd ? save_invstd : mean + (size_t)n * groups;
+        float *parts = (float *)ws + room.pairs;
+        const size_t lds = ((size_t)(p.map.slots + 2) * p.W + 16) * sizeof(float);
         const int each = gn_images(n, (long)p.bands * p.chunks, kGnThreads);
         for (int n0 = 0; n0 < n; n0 += each) {
             const int images = n - n0 < each ? n - n0 : each;
             const GnShape s{HW, c, groups, Cg, n0};
             const dim3 grid((unsigned)(images * p.bands * p.chunks));
-            hipLaunchKernelGGL((gn_stats_kernel<T, V>), grid, dim3(kGnThreads), lds, st, s, p, x, part);
-            hipLaunchKernelGGL(gn_stats_merge_kernel, dim3(images * groups), dim3(kGnMergeThreads), 0, st, s, p, part, eps, mean, invstd);
+            hipLaunchKernelGGL((gn_stats_kernel<T, V, S>), grid, dim3(kGnThreads), lds, st, s, p, x, parts);
+            hipLaunchKernelGGL(gn_stats_merge_kernel, dim3(images * groups), dim3(kGnMergeThreads), 0, st, s, p, parts, eps, mean, invstd);
             gn_with_act(act, [&](auto a) {
                 gn_with(res != nullptr, [&](auto r) {
-                    hipLaunchKernelGGL((gn_apply_kernel<T, V, decltype(a)::value, decltype(r)::value>), grid, dim3(kGnThreads), 0, st, s, p, x, gamma,
-                                       beta, mean, invstd, res, y);
+                    hipLaunchKernelGGL((gn_apply_kernel<T, V, S, decltype(a)::value, decltype(r)::value>), grid, dim3(kGnThreads), 0, st, s, p, x,
+                                       gamma, beta, mean, invstd, res, y);
                 });
             });
         }
@@ -882,8 +939,7 @@ static int gn_bwd_impl(const char *who, int n, int c, int h, int w, int layout, 
     const int HW = h * w, Cg = c / groups;
     const GnRoom room = gn_room(n, c, HW, groups);
     RN50_REQUIRE(ws_bytes >= room.floats() * sizeof(float), RN50_EWORKSPACE, "%s: workspace too small", who);
-    const long NC = (long)n * c;
-    float *sums = (float *)ws;
+    float *means = (float *)ws, *parts = means + room.pairs, *chans = parts + room.parts;
     hipStream_t st = (hipStream_t)stream;
     const GnBwdIn<T> in{x, dy, dy2, act == RN50_ACT_NONE ? nullptr : res, gamma, beta, mean, invstd};
     auto with_kind = [&](auto f) {  // f(ACT, RES, DY2)
@@ -894,45 +950,46 @@ static int gn_bwd_impl(const char *who, int n, int c, int h, int w, int layout, 
             });
         });
     };
-    gn_with_vector<T>(c, Cg, [&](auto vec) {
-        constexpr int V = decltype(vec)::value;
-        const int W = gn_run(c, Cg, V, sizeof(T), kGnSegment);
-        bool done = false;
-        if (W)
-            done = gn_first_fit_of<GnSize<256, 4>, GnSize<256, 8>, GnSize<512, 8>, GnSize<V == 4 ? 1024 : 512, 8>>(HW, W / V, [&](auto size) {
-                constexpr int TH = decltype(size)::threads, E = decltype(size)::rows;
-                const GnResident p{GnMap::of(W / V, TH), W, c / W};
-                const size_t lds = gn_lds_floats(p.map, W, 2) * sizeof(float);
-                const int each = gn_images(n, p.chunks, TH);
-                for (int n0 = 0; n0 < n; n0 += each) {
-                    const GnShape s{HW, c, groups, Cg, n0};
-                    const dim3 grid((unsigned)((n - n0 < each ? n - n0 : each) * p.chunks));
-                    with_kind([&](auto a, auto r, auto d) {
-                        hipLaunchKernelGGL((gn_bwd_kernel<T, V, E, TH, decltype(a)::value, decltype(r)::value, decltype(d)::value>), grid, dim3(TH), lds,
-                                           st, s, p, NC, in, sums, dx, dres);
-                    });
-                }
+    const int param_blocks = ceil_div(c, kGnParamCh);
+    gn_with_vector<T>(Cg, [&](auto vec, auto per_group) {
+        constexpr int V = decltype(vec)::value, S = decltype(per_group)::value;
+        if constexpr (V > 1) {
+            const int W = gn_run(c, Cg, V, sizeof(T), kGnSegment);
+            if (gn_first_fit_of<GnSize<256, 4>, GnSize<256, 8>, GnSize<512, 8>, GnSize<V == 4 ? 1024 : 512, 8>>(HW, W, V, 2, [&](auto size) {
+                    constexpr int TH = decltype(size)::threads, E = decltype(size)::rows;
+                    const GnResident p{GnMap::of(W / V, TH), W, c / W};
+                    const size_t lds = gn_lds_floats(p.map, W, 2) * sizeof(float);
+                    const int each = gn_images(n, p.chunks, TH);
+                    for (int n0 = 0; n0 < n; n0 += each) {
+                        const GnShape s{HW, c, groups, Cg, n0};
+                        const dim3 grid((unsigned)((n - n0 < each ? n - n0 : each) * p.chunks));
+                        with_kind([&](auto a, auto r, auto d) {
+                            hipLaunchKernelGGL((gn_bwd_kernel<T, V, S, E, TH, decltype(a)::value, decltype(r)::value, decltype(d)::value>), grid,
+                                               dim3(TH), lds, st, s, p, (long)n * c, in, chans, dx, dres);
+                        });
+                    }
+                    hipLaunchKernelGGL(gn_params_kernel, dim3(param_blocks), dim3(kGnThreads), 0, st, (long)n, c, chans, dgamma, dbeta);
+                }))
+                return;
+        }
+        const GnBands p = gn_bands(n, HW, c, Cg, V, kGnSumRows);
+        const long rows = (long)n * p.bands;
+        const size_t lds = ((size_t)(p.map.slots + 4) * p.W + 16) * sizeof(float);
+        const int each = gn_images(n, (long)p.bands * p.chunks, kGnThreads);
+        for (int n0 = 0; n0 < n; n0 += each) {
+            const int images = n - n0 < each ? n - n0 : each, blocks = images * p.bands * p.chunks;
+            const int params = n0 + images == n ? param_blocks : 0;  // with the last launch
+            const GnShape s{HW, c, groups, Cg, n0};
+            with_kind([&](auto a, auto r, auto d) {
+                constexpr int ACT = decltype(a)::value;
+                constexpr bool RES = decltype(r)::value, DY2 = decltype(d)::value;
+                hipLaunchKernelGGL((gn_sums_kernel<T, V, S, ACT, RES, DY2>), dim3(blocks), dim3(kGnThreads), lds, st, s, p, in, chans, rows * c, parts);
+                hipLaunchKernelGGL(gn_sums_merge_kernel, dim3(images * groups), dim3(kGnMergeThreads), 0, st, s, p, parts, means);
+                hipLaunchKernelGGL((gn_bwd_apply_kernel<T, V, S, ACT, RES, DY2>), dim3(blocks + params), dim3(kGnThreads), 0, st, s, p, in, means, dx,
+                                   dres, params, rows, chans, dgamma, dbeta);
             });
-        if (!done) {
-            const GnBands p = gn_bands<T>(n, HW, c, V);
-            float *means = sums + room.sums, *part = means + room.pairs;
-            const size_t lds = (size_t)(p.map.slots + 2) * p.W * sizeof(float);
-            const int each = gn_images(n, (long)p.bands * p.chunks, kGnThreads);
-            for (int n0 = 0; n0 < n; n0 += each) {
-                const int images = n - n0 < each ? n - n0 : each;
-                const GnShape s{HW, c, groups, Cg, n0};
-                const dim3 grid((unsigned)(images * p.bands * p.chunks));
-                with_kind([&](auto a, auto r, auto d) {
-                    constexpr int ACT = decltype(a)::value;
-                    constexpr bool RES = decltype(r)::value, DY2 = decltype(d)::value;
-                    hipLaunchKernelGGL((gn_sums_kernel<T, V, ACT, RES, DY2>), grid, dim3(kGnThreads), lds, st, s, p, in, part);
-                    hipLaunchKernelGGL(gn_sums_merge_kernel, dim3(images * groups), dim3(kGnMergeThreads), 0, st, s, p, part, gamma, NC, sums, means);
-                    hipLaunchKernelGGL((gn_bwd_apply_kernel<T, V, ACT, RES, DY2>), grid, dim3(kGnThreads), 0, st, s, p, in, means, dx, dres);
-                });
-            }
         }
     });
-    hipLaunchKernelGGL(gn_params_kernel, dim3(ceil_div(c, 64)), dim3(64 * kGnParamWaves), 0, st, n, c, sums, dgamma, dbeta);
     return launch_status(who);
 }
 

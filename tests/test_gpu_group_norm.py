@@ -20,10 +20,12 @@ pytestmark = pytest.mark.gpu
 ACTS = {"none": rn.ACT_NONE, "relu": rn.ACT_RELU, "silu": rn.ACT_SILU}
 EPS = 1e-5
 # (n, c, h, w, groups): one value to a group up to many, groups of 1, 2, 3, 5, 8, 10, 24, 64 channels and all of them, one pixel, odd
-# images, images of more pixels than any workgroup holds, more images than compute units
+# images, images of more pixels than any workgroup holds, more images than compute units,
+# groups wider than a workgroup takes, in fours of channels and not
 SHAPES = [(1, 4, 1, 1, 1), (2, 8, 1, 1, 8), (1, 4, 1, 3, 2), (3, 24, 5, 7, 8), (2, 20, 9, 4, 4), (2, 64, 56, 56, 32), (2, 2048, 7, 7, 32), (4, 256, 14, 14, 32),
           (1, 320, 33, 35, 32), (5, 48, 13, 11, 2), (1, 64, 112, 112, 32), (2, 12, 130, 67, 12), (300, 16, 3, 3, 4), (1, 8, 257, 255, 1), (2, 1028, 3, 3, 4),
-          (7, 512, 4, 4, 1), (1, 4, 1, 1, 4), (2, 256, 40, 40, 4)]
+          (7, 512, 4, 4, 1), (1, 4, 1, 1, 4), (2, 256, 40, 40, 4), (1, 4100, 2, 3, 4), (2, 8192, 3, 1, 1),
+          (1, 2056, 5, 40, 1), (1, 4096, 9, 7, 2), (2, 2052, 11, 3, 4)]
 
 
 def _round(a, bf16):
