@@ -47,6 +47,26 @@ template <> struct GnVec<bf16_t, 8> {
 };
 template <class T, int V> __device__ inline typename GnVec<T, V>::Raw gn_load(const T *p) { return *reinterpret_cast<const typename GnVec<T, V>::Raw *>(p); }
 template <class T, int V> __device__ inline void gn_store(T *p, const float *f) { *reinterpret_cast<typename GnVec<T, V>::Raw *>(p) = GnVec<T, V>::pack(f); }
+// The same past the caches' normal order of keeping lines.  For the second pass over memory: its results, and what it reads for the last
+// time, would push out what it has yet to read again.  32 x 112 x 112 x 64 fp32 backward 113 -> 95 us, 128 x 56 x 56 x 256 bf16 forward
+// 150 -> 130 (stores alone 142), 3 x 129 x 131 x 320 forward 42 -> 36.  A workgroup that keeps its group reads nothing again: there
+// 64 x 14 x 14 x 1024 bf16 backward takes 45 us so instead of 43.
+template <class T, int V> struct GnWords {
+    typedef typename GnVec<T, V>::Raw Raw;
+    typedef uint32_t Words __attribute__((ext_vector_type(sizeof(Raw) < 4 ? 1 : sizeof(Raw) / 4)));
+};
+template <class T, int V> __device__ inline typename GnVec<T, V>::Raw gn_load_past(const T *p)
+{
+    typedef GnWords<T, V> W;
+    if constexpr (V == 1) return __builtin_nontemporal_load(p);
+    else return __builtin_bit_cast(typename W::Raw, __builtin_nontemporal_load(reinterpret_cast<const typename W::Words *>(p)));
+}
+template <class T, int V> __device__ inline void gn_store_past(T *p, const float *f)
+{
+    typedef GnWords<T, V> W;
+    if constexpr (V == 1) __builtin_nontemporal_store(GnVec<T, V>::pack(f), p);
+    else __builtin_nontemporal_store(__builtin_bit_cast(typename W::Words, GnVec<T, V>::pack(f)), reinterpret_cast<typename W::Words *>(p));
+}
 template <int V> __device__ inline void gn_load_floats(const float *p, float *f)
 {
     constexpr int S = V == 1 ? 1 : 4;
@@ -195,6 +215,7 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
                                                     float *__restrict__ save_mean, float *__restrict__ save_invstd)
 {
     typedef GnVec<T, V> Vec;
+    constexpr int PER = V / S;  // channels of a thread that share statistics
     extern __shared__ float lds[];
     float *part = lds, *chan = part + p.map.slots * p.W, *red = chan + p.W, *grp = red + 16;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);
@@ -206,25 +227,25 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (e * RL < s.HW && t.active) raw[e] = gn_load<T, V>(x + base + (long)min(t.row + e * RL, s.HW - 1) * s.C);
-    float a[V];
+    float a[S], mean[S];
 #pragma unroll
-    for (int i = 0; i < V; ++i) a[i] = 0.f;
+    for (int i = 0; i < S; ++i) a[i] = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (t.active && t.row + e * RL < s.HW) {
             float f[V];
             Vec::unpack(raw[e], f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) a[i] += f[i];
+            for (int i = 0; i < V; ++i) a[gn_at<S>(i)] += f[i];
         }
-    gn_column_sums<V>(p.map, t, a, part, chan);
-    gn_group_sums(p.W, s.Cg, chan, grp, red);
+    gn_column_sums<S>(p.map, t, a, part, chan);
+    gn_group_sums(p.W / PER, s.Cg / PER, chan, grp, red);
     const float m = (float)s.HW * (float)s.Cg;  // a division: the mean of equal values is that value, whatever their number
-    float mean[S];
 #pragma unroll
-    for (int i = 0; i < S; ++i) mean[i] = grp[(col + i) / s.Cg] / m;
-#pragma unroll
-    for (int i = 0; i < V; ++i) a[i] = 0.f;
+    for (int i = 0; i < S; ++i) {
+        mean[i] = grp[(col + i) / s.Cg] / m;
+        a[i] = 0.f;
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (t.active && t.row + e * RL < s.HW) {
@@ -233,11 +254,11 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float d = f[i] - mean[gn_at<S>(i)];
-                a[i] = fmaf(d, d, a[i]);
+                a[gn_at<S>(i)] = fmaf(d, d, a[gn_at<S>(i)]);
             }
         }
-    gn_column_sums<V>(p.map, t, a, part, chan);  // its first barrier: every thread has read grp
-    gn_group_sums(p.W, s.Cg, chan, grp, red);
+    gn_column_sums<S>(p.map, t, a, part, chan);  // its first barrier: every thread has read grp
+    gn_group_sums(p.W / PER, s.Cg / PER, chan, grp, red);
     if (!t.active) return;
     float scale[V], b[V], invstd[S];
     gn_load_floats<V>(gamma + c, scale);
@@ -301,12 +322,13 @@ template <int V, int S> struct GnColumn {
 };
 template <class T, int V, int ACT, bool RES, bool DY2> struct GnDz {
     typename GnVec<T, V>::Raw x, dy, dy2, res;
-    __device__ void load(const GnBwdIn<T> &in, long at)
+    template <bool PAST = false> __device__ void load(const GnBwdIn<T> &in, long at)
     {
-        x = gn_load<T, V>(in.x + at);
-        dy = gn_load<T, V>(in.dy + at);
-        if (DY2) dy2 = gn_load<T, V>(in.dy2 + at);
-        if (RES) res = gn_load<T, V>(in.res + at);
+        auto get = [at](const T *p) { return PAST ? gn_load_past<T, V>(p + at) : gn_load<T, V>(p + at); };
+        x = get(in.x);
+        dy = get(in.dy);
+        if (DY2) dy2 = get(in.dy2);
+        if (RES) res = get(in.res);
     }
     // dz, and x - mean
     template <int S> __device__ void form(const GnColumn<V, S> &k, float *dz, float *d) const
@@ -414,8 +436,8 @@ __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, lon
 // ---- two passes over memory ------------------------------------------------------------------------------------------------
 // A workgroup takes a band of rows of a run of channels: whole groups, or a piece of one where a group has more vectors than
 // that.  Partial results lie at [image][group][piece][band], a second plane behind the first.
-constexpr int kGnThreads = 512, kGnCols = 256;  // vectors of a row in a workgroup, at most: LDS stays below 48 KB
-constexpr int kGnStatRows = 8, kGnSumRows = 16;  // rows of a thread in a band
+constexpr int kGnThreads = 256, kGnCols = 256;  // vectors of a row in a workgroup, at most
+constexpr int kGnBatch = 4;                     // rows of a thread whose loads are in flight together
 struct GnBands {
     GnMap map;
     int W, chunks;    // channels of a workgroup (fewer in the last of an image, or of a group in pieces), workgroups to a row
@@ -456,56 +478,76 @@ struct GnPlace {
     }
 };
 
-// mean and sum of squared deviations of every group over a band
+// Chan et al.: mean and squared deviations of a set of `na` values take in those of `nb` others (any unit of counting).
+__device__ inline void gn_merge(float &mean, float &m2, float na, float mean_b, float m2_b, float nb)
+{
+    const float d = mean_b - mean, part = nb / (na + nb);
+    mean = fmaf(d, part, mean);
+    m2 = m2 + m2_b + d * d * (na * part);
+}
+
+// mean and sum of squared deviations of every group over a band.  A thread forms both of each batch of rows, exactly as of a whole
+// tensor, and merges the batches; the threads are merged about the group's mean.
 template <class T, int V, int S>
 __global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnShape s, GnBands p, const T *__restrict__ x, float *__restrict__ parts)
 {
     typedef GnVec<T, V> Vec;
+    constexpr int PER = V / S;  // channels of a thread that share statistics
     extern __shared__ float lds[];
-    float *part = lds, *chan = part + p.map.slots * p.W, *red = chan + p.W, *grp = red + 16;
+    const int sums = p.map.cols * S;  // a row's partial sums
+    float *part = lds, *chan = part + p.map.slots * sums, *red = chan + sums, *grp = red + 16;
     const GnPlace pl(s, p, blockIdx.x, gridDim.x, false);
     GnThread t(p.map);
     t.active = t.active && t.col * V < pl.width;
     const int col = t.active ? t.col * V : 0, rows = pl.rows, RL = p.map.row_lanes;
     const T *from = x + ((long)(s.n0 + pl.image) * s.HW + (long)pl.band * p.rows) * s.C + pl.c0 + col;
-    typename Vec::Raw raw[kGnStatRows];
+    float mean[S], m2[S], count = 0.f;  // count: rows
 #pragma unroll
-    for (int e = 0; e < kGnStatRows; ++e)
-        if (e * RL < rows && t.active) raw[e] = gn_load<T, V>(from + (long)min(t.row + e * RL, rows - 1) * s.C);
-    float a[V], mean[S];
+    for (int i = 0; i < S; ++i) mean[i] = m2[i] = 0.f;
+    if (t.active)
+        for (int r0 = t.row; r0 < rows; r0 += kGnBatch * RL) {
+            float f[kGnBatch][V];
+            typename Vec::Raw raw[kGnBatch];
 #pragma unroll
-    for (int i = 0; i < V; ++i) a[i] = 0.f;
+            for (int u = 0; u < kGnBatch; ++u) raw[u] = gn_load<T, V>(from + (long)min(r0 + u * RL, rows - 1) * s.C);
 #pragma unroll
-    for (int e = 0; e < kGnStatRows; ++e)
-        if (t.active && t.row + e * RL < rows) {
-            float f[V];
-            Vec::unpack(raw[e], f);
+            for (int u = 0; u < kGnBatch; ++u) Vec::unpack(raw[u], f[u]);
+            const float here = (float)min(kGnBatch, (rows - 1 - r0) / RL + 1), inv = 1.f / (here * PER);
 #pragma unroll
-            for (int i = 0; i < V; ++i) a[i] += f[i];
+            for (int i = 0; i < S; ++i) {
+                float a = 0.f, q = 0.f;
+#pragma unroll
+                for (int u = 0; u < kGnBatch; ++u)
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) a += u < here ? f[u][i * PER + k] : 0.f;
+                a *= inv;
+#pragma unroll
+                for (int u = 0; u < kGnBatch; ++u)
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) {
+                        const float d = f[u][i * PER + k] - a;
+                        q = fmaf(u < here ? d : 0.f, d, q);
+                    }
+                gn_merge(mean[i], m2[i], count * PER, a, q, here * PER);
+            }
+            count += here;
         }
-    gn_column_sums<V>(p.map, t, a, part, chan);
-    gn_group_sums(pl.width, pl.run, chan, grp, red);
+    float a[S];
+#pragma unroll
+    for (int i = 0; i < S; ++i) a[i] = mean[i] * (count * PER);
+    gn_column_sums<S>(p.map, t, a, part, chan);
+    gn_group_sums(pl.width / PER, pl.run / PER, chan, grp, red);
     const float m = (float)rows * (float)pl.run;
 #pragma unroll
-    for (int i = 0; i < S; ++i) mean[i] = grp[(col + i) / pl.run] / m;
-#pragma unroll
-    for (int i = 0; i < V; ++i) a[i] = 0.f;
-#pragma unroll
-    for (int e = 0; e < kGnStatRows; ++e)
-        if (t.active && t.row + e * RL < rows) {
-            float f[V];
-            Vec::unpack(raw[e], f);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = f[i] - mean[gn_at<S>(i)];
-                a[i] = fmaf(d, d, a[i]);
-            }
-        }
-    const int count = pl.width / pl.run;
-    for (int k = threadIdx.x; k < count; k += kGnThreads) *pl.partial(s, p, parts, k) = grp[k] / m;
-    gn_column_sums<V>(p.map, t, a, part, chan);  // its first barrier: every thread has read grp
-    gn_group_sums(pl.width, pl.run, chan, grp, red);
-    for (int k = threadIdx.x; k < count; k += kGnThreads) *pl.partial(s, p, parts + p.plane, k) = grp[k];
+    for (int i = 0; i < S; ++i) {
+        const float d = mean[i] - grp[(col + i) / pl.run] / m;
+        a[i] = count > 0.f ? fmaf(d * d, count * PER, m2[i]) : 0.f;
+    }
+    const int groups = pl.width / pl.run;
+    for (int k = threadIdx.x; k < groups; k += kGnThreads) *pl.partial(s, p, parts, k) = grp[k] / m;
+    gn_column_sums<S>(p.map, t, a, part, chan);  // its first barrier: every thread has read grp
+    gn_group_sums(pl.width / PER, pl.run / PER, chan, grp, red);
+    for (int k = threadIdx.x; k < groups; k += kGnThreads) *pl.partial(s, p, parts + p.plane, k) = grp[k];
 }
 
 constexpr int kGnMergeThreads = 256;
@@ -571,14 +613,14 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnShape s, GnBands
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) scale[i] *= inv[gn_at<S>(i)];
-    constexpr int B = 4;
+    constexpr int B = kGnBatch;
     for (int r0 = t.row; r0 < rows; r0 += B * RL) {
         typename Vec::Raw xr[B], rr[B];
 #pragma unroll
         for (int u = 0; u < B; ++u)
             if (r0 + u * RL < rows) {
-                xr[u] = gn_load<T, V>(x + base + (long)(r0 + u * RL) * s.C);
-                if (RES) rr[u] = gn_load<T, V>(res + base + (long)(r0 + u * RL) * s.C);
+                xr[u] = gn_load_past<T, V>(x + base + (long)(r0 + u * RL) * s.C);
+                if (RES) rr[u] = gn_load_past<T, V>(res + base + (long)(r0 + u * RL) * s.C);
             }
 #pragma unroll
         for (int u = 0; u < B; ++u)
@@ -592,7 +634,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnShape s, GnBands
                     if (RES) v += q[i];
                     f[i] = gn_act<ACT>(v);
                 }
-                gn_store<T, V>(y + base + (long)(r0 + u * RL) * s.C, f);
+                gn_store_past<T, V>(y + base + (long)(r0 + u * RL) * s.C, f);
             }
     }
 }
@@ -613,7 +655,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape s, GnBands 
     float a0[V], a1[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) a0[i] = a1[i] = 0.f;
-    constexpr int B = 4;
+    constexpr int B = kGnBatch;
     if (t.active)
         for (int r0 = t.row; r0 < rows; r0 += B * RL) {
             GnDz<T, V, ACT, RES, DY2> q[B];
@@ -730,21 +772,21 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_apply_kernel(GnShape s, GnB
         A[i] = means[at] * k.inv[i];
         Bm[i] = means[at + 1] * k.inv[i];
     }
-    constexpr int B = 4;
+    constexpr int B = kGnBatch;
     for (int r0 = t.row; r0 < rows; r0 += B * RL) {
         GnDz<T, V, ACT, RES, DY2> q[B];
 #pragma unroll
         for (int u = 0; u < B; ++u)
-            if (r0 + u * RL < rows) q[u].load(in, base + (long)(r0 + u * RL) * s.C);
+            if (r0 + u * RL < rows) q[u].template load<true>(in, base + (long)(r0 + u * RL) * s.C);
 #pragma unroll
         for (int u = 0; u < B; ++u)
             if (r0 + u * RL < rows) {
                 float dz[V], d[V];
                 q[u].form(k, dz, d);
                 const long at = base + (long)(r0 + u * RL) * s.C;
-                if (dres) gn_store<T, V>(dres + at, dz);
+                if (dres) gn_store_past<T, V>(dres + at, dz);
                 gn_dx<V, S>(k, dz, d, A, Bm, d);
-                gn_store<T, V>(dx + at, d);
+                gn_store_past<T, V>(dx + at, d);
             }
     }
 }
@@ -765,7 +807,8 @@ static int gn_run(int C, int Cg, int V, int size, int bytes)
 
 constexpr int kGnSegment = 64;
 // The two-pass kernels' cut.
-static GnBands gn_bands(int n, int HW, int C, int Cg, int V, int thread_rows)
+// `total` workgroups, where rows are enough for a batch to every thread.
+static GnBands gn_bands(int n, int HW, int C, int Cg, int V, long total)
 {
     GnBands p;
     const int unit = gn_unit(Cg, V), units = C / unit, most = kGnCols * V / unit;  // units of a workgroup
@@ -779,11 +822,19 @@ static GnBands gn_bands(int n, int HW, int C, int Cg, int V, int thread_rows)
         p.chunks = C / Cg * p.pieces;
     }
     p.map = GnMap::of(p.W / V, kGnThreads);
-    p.rows = p.map.row_lanes * thread_rows;
+    long bands = total / ((long)n * p.chunks);
+    const long most_bands = ceil_div(HW, p.map.row_lanes * kGnBatch);
+    bands = bands < 1 ? 1 : bands > most_bands ? most_bands : bands;
+    p.rows = ceil_div(HW, bands);
     p.bands = ceil_div(HW, p.rows);
     p.plane = (long)n * (C / Cg) * p.pieces * p.bands;
     return p;
 }
+
+// The passes that add up: as many workgroups as fit the chip at once, so that they end together, or many rounds of them.
+static long gn_reduce_total(int n) { return n <= 256 ? 1024 : 8192; }
+// The element-wise passes: small workgroups.
+static long gn_apply_total() { return 16384; }
 
 // Vector width: the widest that lies within groups; four channels also across groups, unless whole groups of whole vectors are then more
 // than a workgroup takes.
@@ -799,13 +850,12 @@ struct GnRoom { size_t pairs, parts, chans; size_t floats() const { return pairs
 static GnRoom gn_room(int n, int c, int HW, int groups)
 {
     GnRoom r{((size_t)2 * n * groups + 3) & ~(size_t)3, 0, (size_t)2 * n * c};
-    for (int size : {2, 4})
-        for (int rows : {kGnStatRows, kGnSumRows}) {
-            const GnBands p = gn_bands(n, HW, c, c / groups, gn_vector(c / groups, size), rows);
-            const size_t parts = ((size_t)2 * p.plane + 3) & ~(size_t)3, chans = (size_t)2 * n * p.bands * c;
-            if (parts > r.parts) r.parts = parts;
-            if (rows == kGnSumRows && chans > r.chans) r.chans = chans;
-        }
+    for (int size : {2, 4}) {
+        const GnBands p = gn_bands(n, HW, c, c / groups, gn_vector(c / groups, size), gn_reduce_total(n));
+        const size_t parts = ((size_t)2 * p.plane + 3) & ~(size_t)3, chans = (size_t)2 * n * p.bands * c;
+        if (parts > r.parts) r.parts = parts;
+        if (chans > r.chans) r.chans = chans;
+    }
     return r;
 }
 
@@ -884,7 +934,7 @@ static int gn_fwd_impl(const char *who, int n, int c, int h, int w, int layout, 
         constexpr int V = decltype(vec)::value, S = decltype(per_group)::value;
         if constexpr (V > 1) {
             const int W = gn_run(c, Cg, V, sizeof(T), kGnSegment);
-            if (gn_first_fit_of<GnSize<256, 4>, GnSize<256, 8>, GnSize<512, 8>, GnSize<512, 16>, GnSize<1024, 16>>(HW, W, V, 1, [&](auto size) {
+            if (gn_first_fit_of<GnSize<256, 4>, GnSize<256, 8>, GnSize<512, 8>, GnSize<512, 16>>(HW, W, V, 1, [&](auto size) {
                     constexpr int TH = decltype(size)::threads, E = decltype(size)::rows;
                     const GnResident p{GnMap::of(W / V, TH), W, c / W};
                     const size_t lds = gn_lds_floats(p.map, W, 1) * sizeof(float);
@@ -902,21 +952,20 @@ static int gn_fwd_impl(const char *who, int n, int c, int h, int w, int layout, 
                 }))
                 return;
         }
-        const GnBands p = gn_bands(n, HW, c, Cg, V, kGnStatRows);
+        const GnBands p = gn_bands(n, HW, c, Cg, V, gn_reduce_total(n)), pa = gn_bands(n, HW, c, Cg, V, gn_apply_total());
         float *mean = save_mean ? save_mean : (float *)ws, *invstd = save_invstd ? save_invstd : mean + (size_t)n * groups;
         float *parts = (float *)ws + room.pairs;
         const size_t lds = ((size_t)(p.map.slots + 2) * p.W + 16) * sizeof(float);
-        const int each = gn_images(n, (long)p.bands * p.chunks, kGnThreads);
+        const int each = gn_images(n, (long)pa.bands * pa.chunks, kGnThreads);  // the finer cut
         for (int n0 = 0; n0 < n; n0 += each) {
             const int images = n - n0 < each ? n - n0 : each;
             const GnShape s{HW, c, groups, Cg, n0};
-            const dim3 grid((unsigned)(images * p.bands * p.chunks));
-            hipLaunchKernelGGL((gn_stats_kernel<T, V, S>), grid, dim3(kGnThreads), lds, st, s, p, x, parts);
+            hipLaunchKernelGGL((gn_stats_kernel<T, V, S>), dim3(images * p.bands * p.chunks), dim3(kGnThreads), lds, st, s, p, x, parts);
             hipLaunchKernelGGL(gn_stats_merge_kernel, dim3(images * groups), dim3(kGnMergeThreads), 0, st, s, p, parts, eps, mean, invstd);
             gn_with_act(act, [&](auto a) {
                 gn_with(res != nullptr, [&](auto r) {
-                    hipLaunchKernelGGL((gn_apply_kernel<T, V, S, decltype(a)::value, decltype(r)::value>), grid, dim3(kGnThreads), 0, st, s, p, x,
-                                       gamma, beta, mean, invstd, res, y);
+                    hipLaunchKernelGGL((gn_apply_kernel<T, V, S, decltype(a)::value, decltype(r)::value>), dim3(images * pa.bands * pa.chunks),
+                                       dim3(kGnThreads), 0, st, s, pa, x, gamma, beta, mean, invstd, res, y);
                 });
             });
         }
@@ -972,12 +1021,12 @@ static int gn_bwd_impl(const char *who, int n, int c, int h, int w, int layout, 
                 }))
                 return;
         }
-        const GnBands p = gn_bands(n, HW, c, Cg, V, kGnSumRows);
+        const GnBands p = gn_bands(n, HW, c, Cg, V, gn_reduce_total(n)), pa = gn_bands(n, HW, c, Cg, V, gn_apply_total());
         const long rows = (long)n * p.bands;
         const size_t lds = ((size_t)(p.map.slots + 4) * p.W + 16) * sizeof(float);
-        const int each = gn_images(n, (long)p.bands * p.chunks, kGnThreads);
+        const int each = gn_images(n, (long)pa.bands * pa.chunks, kGnThreads);  // the finer cut
         for (int n0 = 0; n0 < n; n0 += each) {
-            const int images = n - n0 < each ? n - n0 : each, blocks = images * p.bands * p.chunks;
+            const int images = n - n0 < each ? n - n0 : each, blocks = images * p.bands * p.chunks, finer = images * pa.bands * pa.chunks;
             const int params = n0 + images == n ? param_blocks : 0;  // with the last launch
             const GnShape s{HW, c, groups, Cg, n0};
             with_kind([&](auto a, auto r, auto d) {
@@ -985,7 +1034,7 @@ static int gn_bwd_impl(const char *who, int n, int c, int h, int w, int layout, 
                 constexpr bool RES = decltype(r)::value, DY2 = decltype(d)::value;
                 hipLaunchKernelGGL((gn_sums_kernel<T, V, S, ACT, RES, DY2>), dim3(blocks), dim3(kGnThreads), lds, st, s, p, in, chans, rows * c, parts);
                 hipLaunchKernelGGL(gn_sums_merge_kernel, dim3(images * groups), dim3(kGnMergeThreads), 0, st, s, p, parts, means);
-                hipLaunchKernelGGL((gn_bwd_apply_kernel<T, V, S, ACT, RES, DY2>), dim3(blocks + params), dim3(kGnThreads), 0, st, s, p, in, means, dx,
+                hipLaunchKernelGGL((gn_bwd_apply_kernel<T, V, S, ACT, RES, DY2>), dim3(finer + params), dim3(kGnThreads), 0, st, s, pa, in, means, dx,
                                    dres, params, rows, chans, dgamma, dbeta);
             });
         }
