@@ -421,8 +421,8 @@ int softmax_ce(int n, int k, const float *logits, const int32_t *labels, float *
 #define RN50_TOPK_MAX 256
 
 /* val[n][0..t), idx[n][0..t): the t largest logits of each row (t <= K) and their classes, in falling order; equal logits
- * by rising class (-0 and 0 are equal).  A NaN counts as larger than any number, as all of them equal.  Values are the
- * logits themselves, widened exactly. */
+ * by rising class (-0 and 0 are equal; both are given as 0).  A NaN counts as larger than any number, and all of them as equal.
+ * Values are the logits themselves, widened exactly.  Rows longer than 2^15 * floor(6144 / t) classes: RN50_EUNSUPPORTED. */
 size_t rn50_topk_workspace_bytes(int n, int k, int t);
 int logits_topk(int n, int k, int t, const float *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes, void *stream);
 int logits_topk_bf16(int n, int k, int t, const uint16_t *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes,

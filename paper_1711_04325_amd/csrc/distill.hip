@@ -1,66 +1,10 @@
-// Learning from a teacher's largest logits (Hinton et al. 2015): picking them from rows of logits, and the cross-entropy with the label
-// and with them, with its gradient.
-#include "common.h"
+// Learning from a teacher's largest logits (Hinton et al. 2015): the cross-entropy with the label and with them, with its gradient.
+#include "rows.h"
 
 namespace rn50 {
 
 constexpr int kRowThreads = 256;
-constexpr int kMaxRows = 1 << 22;  // a launch has fewer than 2^32 threads
 
-__device__ inline float row_ld(const float *p, long i) { return p[i]; }
-__device__ inline float row_ld(const bf16_t *p, long i) { return __uint_as_float((uint32_t)p[i] << 16); }
-__device__ inline void row_st(float *p, long i, float v) { p[i] = v; }
-__device__ inline void row_st(bf16_t *p, long i, float v) { p[i] = (bf16_t)bf16_rne(v); }
-
-// ---- the t largest of a row ----------------------------------------------------------------------------------------------
-// A logit and its class as one number: larger logits first, then smaller classes, so that no two elements of a row are equal.  The upper
-// half orders floats as integers do (negative numbers with their lower 31 bits turned round), -0 with 0 and all NaNs at the top.
-__device__ inline uint64_t topk_key(float v, int k)
-{
-    const uint32_t b = __float_as_uint(v + 0.f);  // -0 + 0 = 0
-    const uint32_t o = v != v ? 0xffffffffu : b & 0x80000000u ? ~b : b | 0x80000000u;
-    return (uint64_t)o << 32 | (0xffffffffu - (uint32_t)k);
-}
-__device__ inline int topk_class(uint64_t key) { return (int)(0xffffffffu - (uint32_t)key); }
-
-__device__ inline uint64_t wave_max64(uint64_t v)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const uint64_t w = __shfl_xor((unsigned long long)v, o, 64);
-        v = w > v ? w : v;
-    }
-    return v;
-}
-
-template <class T>
-__global__ __launch_bounds__(kRowThreads) void topk_kernel(int K, int t, const T *__restrict__ z, size_t ld, float *__restrict__ val,
-                                                           int32_t *__restrict__ idx)
-{
-    __shared__ uint64_t red[kRowThreads / 64];
-    const T *row = z + blockIdx.x * ld;
-    uint64_t last = ~0ull;  // above every key: a NaN's lower half is at most 2^32 - 1, that of class 0, which the first round may take
-    for (int i = 0; i < t; ++i) {
-        uint64_t best = 0;
-        for (int k = threadIdx.x; k < K; k += kRowThreads) {
-            const uint64_t key = topk_key(row_ld(row, k), k);
-            if ((i == 0 || key < last) && key > best) best = key;
-        }
-        best = wave_max64(best);
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = best;
-        __syncthreads();
-        for (int w = 0; w < kRowThreads / 64; ++w) best = red[w] > best ? red[w] : best;
-        last = best;
-        if (threadIdx.x == 0) {
-            const int k = topk_class(best);
-            val[(size_t)blockIdx.x * t + i] = row_ld(row, k);
-            idx[(size_t)blockIdx.x * t + i] = k;
-        }
-    }
-}
-
-// ---- distillation --------------------------------------------------------------------------------------------------------
 template <class Op>
 __device__ inline float row_reduce(float v, float *red, Op op)
 {
@@ -201,22 +145,6 @@ __global__ __launch_bounds__(kRowThreads) void distill_loss_kernel(int N, float 
 static size_t distill_ws_bytes(int n) { return (size_t)2 * n * sizeof(float); }
 
 template <class T>
-static int topk_impl(const char *who, int n, int k, int t, const T *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes,
-                     void *stream)
-{
-    RN50_REQUIRE(n > 0 && k > 0 && t > 0, RN50_EINVAL, "%s: non-positive dimension", who);
-    RN50_REQUIRE(n < kMaxRows, RN50_EUNSUPPORTED, "%s: 2^22 rows and more", who);
-    RN50_REQUIRE(t <= k, RN50_EINVAL, "%s: more logits asked for than a row has", who);
-    RN50_REQUIRE(t <= RN50_TOPK_MAX, RN50_EUNSUPPORTED, "%s: at most %d logits of a row", who, RN50_TOPK_MAX);
-    RN50_REQUIRE(ld >= (size_t)k && ld < (1ull << 31), RN50_EINVAL, "%s: rows overlap or are 2^31 elements apart and more", who);
-    RN50_REQUIRE(logits && val && idx, RN50_EINVAL, "%s: null pointer", who);
-    RN50_REQUIRE(aligned16(logits) && aligned16(val) && aligned16(idx) && aligned16(ws), RN50_EINVAL, "%s: pointers must be 16-byte aligned", who);
-    (void)ws_bytes;
-    hipLaunchKernelGGL((topk_kernel<T>), dim3(n), dim3(kRowThreads), 0, (hipStream_t)stream, k, t, logits, ld, val, idx);
-    return launch_status(who);
-}
-
-template <class T>
 static int distill_impl(const char *who, int n, int k, int t, const T *logits, size_t ld, const int32_t *labels, const int32_t *teacher_idx,
                         const float *teacher_val, float alpha, float tau, float scale, float *loss, T *dlogits, size_t ld_d, void *ws,
                         size_t ws_bytes, void *stream)
@@ -249,18 +177,6 @@ static int distill_impl(const char *who, int n, int k, int t, const T *logits, s
 }  // namespace rn50
 
 using namespace rn50;
-
-extern "C" size_t rn50_topk_workspace_bytes(int, int, int) { return 0; }
-
-extern "C" int logits_topk(int n, int k, int t, const float *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes, void *stream)
-{
-    return topk_impl<float>("logits_topk", n, k, t, logits, ld, val, idx, ws, ws_bytes, stream);
-}
-extern "C" int logits_topk_bf16(int n, int k, int t, const uint16_t *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes,
-                                void *stream)
-{
-    return topk_impl<bf16_t>("logits_topk_bf16", n, k, t, logits, ld, val, idx, ws, ws_bytes, stream);
-}
 
 extern "C" size_t rn50_distill_workspace_bytes(int n, int k, int t)
 {

@@ -1,0 +1,382 @@
+// The t largest logits of each row, in order.  One pass over memory: a workgroup keeps its part of a row in registers and finds a bound
+// that at least t elements reach and few more.  Every wavefront's r-th largest of its lanes' own maxima, r = t / wavefronts, is reached by
+// r elements there; the smallest of these bounds over the wavefronts by t in all.  (Random rows of 32768 and t = 64: some 110 elements.)
+// Those go to LDS, and each counts how many are larger: that is its place.
+// Where too many reach the bound (equal logits, rows made to defeat it), the t-th largest element itself is found bit by bit.
+// Long rows of which there are few are cut into parts for several workgroups, and the parts' sorted lists merged.
+#include "rows.h"
+
+namespace rn50 {
+
+// ---- logits as integers ----------------------------------------------------------------------------------------------------
+// Positive floats order as their bits do, and every negative number's bits are a negative integer: a bound above 0 needs no more.  (A NaN
+// with the sign bit set, which belongs at the top, is the one exception; the unsigned maximum of a row's bits shows it.)  For bounds of 0
+// and below, topk_order: 1 for -infinity, rising with the value, -0 with 0, all NaNs together at the top; 0: no element.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+constexpr uint32_t kTopkNan = 0xff000002u;  // order of a NaN
+__device__ inline uint32_t topk_order(uint32_t bits)
+{
+    const uint32_t sign = (uint32_t)((int32_t)bits >> 31), k = ((bits & 0x7fffffffu) ^ sign) - sign;  // the magnitude, negated or not
+    return min(k + 0x7f800000u, kTopkNan - 1) + 1;  // a NaN of either sign lies above +infinity's 0xff000000, a negative one by wrapping round
+}
+__device__ inline uint32_t topk_order2(uint32_t two)  // two bf16 at once, 16 bits each
+{
+    const u16x2 b = __builtin_bit_cast(u16x2, two);
+    const u16x2 sign = __builtin_bit_cast(u16x2, __builtin_bit_cast(i16x2, two) >> 15);
+    const u16x2 k = ((b & (uint16_t)0x7fff) ^ sign) - sign + (uint16_t)0x7f80;
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(k, (u16x2)(uint16_t)0xff01) + (uint16_t)1);
+}
+__device__ inline float topk_value(uint32_t order)
+{
+    const uint32_t k = order - 1 - 0x7f800000u;
+    return order == kTopkNan ? __builtin_nanf("") : __uint_as_float((int32_t)k < 0 ? (0u - k) | 0x80000000u : k);
+}
+// A lane's 16-byte vector is four words, of one fp32 or two bf16 each.  bits(): an element's as those of an fp32 number (a bf16 number is the
+// upper half of one).  Signed integers all the way: in_order() turns a word's elements into their order with the upper bit turned, of_order()
+// gives such an element's topk_order.
+template <class T> struct TopkWord;
+template <> struct TopkWord<float> {
+    typedef uint32_t Int;
+    static constexpr int PER = 1, LOW_BIT = 0;  // elements of a word; bits below LOW_BIT are 0
+    static constexpr uint32_t kNone = 0x80000000u;  // a word without elements: the smallest integer, also of an order of 0
+    static __device__ uint32_t bits(uint32_t w, int) { return w; }
+    static __device__ uint32_t in_order(uint32_t w) { return topk_order(w) ^ kNone; }
+    static __device__ uint32_t of_order(uint32_t bits) { return bits ^ kNone; }
+    static __device__ uint32_t order(float v) { return topk_order(__float_as_uint(v)); }
+    static __device__ uint32_t max_signed(uint32_t a, uint32_t b) { return (uint32_t)max((int32_t)a, (int32_t)b); }
+    static __device__ uint32_t max_unsigned(uint32_t a, uint32_t b) { return max(a, b); }
+    static __device__ bool any_from(uint32_t w, int32_t L) { return (int32_t)w >= L; }
+};
+template <> struct TopkWord<bf16_t> {
+    typedef uint16_t Int;
+    static constexpr int PER = 2, LOW_BIT = 16;
+    static constexpr uint32_t kNone = 0x80008000u;
+    static __device__ uint32_t bits(uint32_t w, int i) { return i ? w & 0xffff0000u : w << 16; }
+    static __device__ uint32_t in_order(uint32_t w) { return topk_order2(w) ^ kNone; }
+    static __device__ uint32_t of_order(uint32_t bits)
+    {
+        const uint32_t o = bits ^ 0x80000000u;
+        return o == 0xff020000u ? kTopkNan : o - 0xffffu;  // 1 + ((order of 16 bits - 1) << 16)
+    }
+    static __device__ uint32_t order(bf16_t v) { return topk_order((uint32_t)v << 16); }
+    static __device__ uint32_t max_signed(uint32_t a, uint32_t b)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
+    }
+    static __device__ uint32_t max_unsigned(uint32_t a, uint32_t b)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+    }
+    // whether one of two reaches L: the larger of each and L - 1 is not L - 1 (L is above the smallest integer)
+    static __device__ bool any_from(uint32_t w, int32_t L)
+    {
+        const uint32_t below = ((uint32_t)L >> 16) - 1, two = (below & 0xffffu) | below << 16;
+        return max_signed(w, two) != two;
+    }
+};
+// An element and its class as one number, no two of a row equal: larger logits first, then smaller classes.
+__device__ inline uint64_t topk_pair(uint32_t order, uint32_t k) { return (uint64_t)order << 32 | (0xffffffffu - k); }
+__device__ inline int topk_class(uint64_t pair) { return (int)(0xffffffffu - (uint32_t)pair); }
+
+// The r-th largest over the lanes of signed integers whose bits below `low` are 0; the smallest integer where there are not that many.
+__device__ inline int32_t wave_rth_largest(int32_t v, int r, int low)
+{
+    uint32_t L = 0;
+    for (int bit = 31; bit >= low; --bit) {
+        const uint32_t higher = L | 1u << bit;
+        if (__popcll(__ballot(((uint32_t)v ^ 0x80000000u) >= higher)) >= r) L = higher;
+    }
+    return (int32_t)(L ^ 0x80000000u);
+}
+
+constexpr int kTopkFound = 1024;  // elements in LDS
+
+// Of `all` pairs in LDS, f(place, pair) for the t largest; place: as many zeros.  Several threads share the counting where there are
+// fewer pairs than threads.
+template <int TH, class F> __device__ inline void topk_places(int t, int all, const uint64_t *found, int *place, F f)
+{
+    const int span = (all + 63) & ~63, shares = max(1, TH / span), chunk = (all + shares - 1) / shares;
+    for (int i0 = threadIdx.x; i0 < span * shares; i0 += TH) {
+        const int i = i0 % span, from = i0 / span * chunk, to = min(all, from + chunk);
+        if (i < all) {
+            const uint64_t own = found[i];
+            int c = 0;
+#pragma unroll 4
+            for (int j = from; j < to; ++j) c += found[j] > own;
+            if (shares > 1) atomicAdd(&place[i], c);
+            else place[i] = c;
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < all; i += TH)
+        if (place[i] < t) f(place[i], found[i]);
+}
+
+// Part s of row n: `per` elements from s*per (a multiple of the vector).  One part: val and idx; several: pairs, [row][part][t], zeros
+// where a part has fewer than t elements.
+template <class T, int TH, int E>
+__global__ __launch_bounds__(TH) void topk_kernel(int K, int t, int parts, int per, const T *__restrict__ z, size_t ld, float *__restrict__ val,
+                                                  int32_t *__restrict__ idx, uint64_t *__restrict__ pairs)
+{
+    typedef TopkWord<T> Word;
+    constexpr int PER = Word::PER, VEC = 4 * PER, WAVES = TH / 64;
+    __shared__ __align__(16) uint64_t found[kTopkFound];
+    __shared__ int place[kTopkFound];
+    __shared__ int32_t bound[2][WAVES];
+    __shared__ int counts[2][WAVES], total[3];
+    const int n = blockIdx.x / parts, s = blockIdx.x % parts, first = s * per, len = min(per, K - first);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const T *row = z + n * ld + first;
+
+    // the last vector of a part, where it is not whole: one thread's
+    uint4 tail = make_uint4(Word::kNone, Word::kNone, Word::kNone, Word::kNone);
+    if (len % VEC && (len / VEC) % TH == (int)threadIdx.x) {
+        typedef unsigned __int128 Vector;
+        constexpr int BITS = 8 * sizeof(T);
+        const Vector none = __builtin_bit_cast(Vector, tail);
+        Vector v = 0;  // the elements, with the bits of no element turned
+        if (len >= VEC) {  // the last VEC elements without those that are in other vectors
+            v = (__builtin_bit_cast(Vector, row_load16(row + len - VEC)) ^ none) >> (VEC - len % VEC) * BITS;
+        } else {
+            for (int i = len - 1; i >= 0; --i) v = v << BITS | (__builtin_bit_cast(typename Word::Int, row[i]) ^ (typename Word::Int)Word::kNone);
+        }
+        tail = __builtin_bit_cast(uint4, v ^ none);
+    }
+    uint32_t w[E][4];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int at = (e * TH + (int)threadIdx.x) * VEC;
+        uint4 raw = make_uint4(Word::kNone, Word::kNone, Word::kNone, Word::kNone);
+        if (at + VEC <= len) raw = row_load16(row + at);
+        else if (at < len) raw = tail;
+        w[e][0] = raw.x; w[e][1] = raw.y; w[e][2] = raw.z; w[e][3] = raw.w;
+    }
+    if (threadIdx.x < 3) total[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < kTopkFound; i += TH) place[i] = 0;
+    // wavefronts all of whose lanes have a vector (or the first): they make the bound
+    const int full = max(1, min(WAVES, (len + VEC - 1) / VEC / 64)), r = (t + full - 1) / full;
+    int all = kTopkFound + 1;
+    // as they are; then, where that gives no bound above 0, in the order of all numbers
+#pragma unroll 1
+    for (int ordered = 0; ordered < 2; ++ordered) {
+        uint32_t big = Word::kNone, odd = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                big = Word::max_signed(big, w[e][i]);
+                odd = Word::max_unsigned(odd, w[e][i]);
+            }
+        const int32_t top = max((int32_t)Word::bits(big, 0), (int32_t)Word::bits(big, PER - 1));
+        int32_t L = 0x7fffffff;
+        if (wave < full) L = r <= 64 ? wave_rth_largest(top, r, Word::LOW_BIT) : INT32_MIN;
+        // a NaN with its sign bit set
+        if (!ordered && __ballot(max(Word::bits(odd, 0), Word::bits(odd, PER - 1)) > 0xff800000u)) L = INT32_MIN;
+        if (lane == 0) bound[ordered][wave] = L;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) L = min(L, bound[ordered][i]);
+        if (!ordered && L <= 0) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[e][i] = Word::in_order(w[e][i]);
+            // (-0, which stands for no element, is in the order of 0 now)
+            const int whole = len / VEC, rest = len % VEC;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int v = e * TH + (int)threadIdx.x;
+                if (v >= whole)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int there = v == whole ? rest - i * PER : 0;  // elements of the word, if more than 0
+                        if (there <= 0) w[e][i] = Word::kNone;
+                        else if (PER == 2 && there == 1) w[e][i] = (w[e][i] & 0xffffu) | 0x80000000u;
+                    }
+            }
+            continue;
+        }
+        L = max(L, (int32_t)((uint32_t)INT32_MIN + (1u << Word::LOW_BIT)));  // the smallest integer is no element
+        // a thread's class numbers are formed where they are used: known before the loop, they would take a register each
+        uint32_t own = first + threadIdx.x * VEC;
+        asm volatile("" : "+v"(own));
+        if (top >= L)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (Word::any_from(w[e][i], L))
+#pragma unroll
+                        for (int j = 0; j < PER; ++j) {
+                            const uint32_t b = Word::bits(w[e][i], j);
+                            if (PER == 1 || (int32_t)b >= L) {
+                                const int slot = atomicAdd(&total[ordered], 1);
+                                if (slot < kTopkFound)
+                                    found[slot] = topk_pair(ordered ? Word::of_order(b) : topk_order(b), own + (e * TH * VEC + i * PER + j));
+                            }
+                        }
+        __syncthreads();
+        all = total[ordered];
+        break;
+    }
+    if (all > kTopkFound) {
+        // too many: the t-th largest element's order, then its place among the equal ones, by counting over the row again and again.
+        // (A part with fewer than t elements has no more than fit, and does not come here.)
+        int turn = 0;
+        auto count = [&](auto reached) {
+            int c = 0;
+            for (int i = threadIdx.x; i < len; i += TH) c += reached(Word::order(row[i]), (uint32_t)i);
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+            if (lane == 0) counts[turn][wave] = c;
+            __syncthreads();
+            c = 0;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) c += counts[turn][i];
+            turn ^= 1;
+            return c;
+        };
+        uint32_t L = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t higher = L | 1u << bit;
+            if (count([&](uint32_t o, uint32_t) { return o >= higher; }) >= t) L = higher;
+        }
+        const int need = t - count([&](uint32_t o, uint32_t) { return o > L; });
+        uint32_t last = 0, hi = (uint32_t)len - 1;  // of the elements equal to L, those up to place `last`
+        while (last < hi) {
+            const uint32_t mid = (last + hi) / 2;
+            if (count([&](uint32_t o, uint32_t k) { return o == L && k <= mid; }) >= need) hi = mid;
+            else last = mid + 1;
+        }
+        for (int i = threadIdx.x; i < len; i += TH) {
+            const uint32_t o = Word::order(row[i]);
+            if (o > L || (o == L && (uint32_t)i <= last)) found[atomicAdd(&total[2], 1)] = topk_pair(o, first + i);
+        }
+        __syncthreads();
+        all = t;
+    }
+    topk_places<TH>(t, all, found, place, [&](int p, uint64_t pair) {
+        if (parts > 1) {
+            pairs[((size_t)n * parts + s) * t + p] = pair;
+        } else {
+            val[(size_t)n * t + p] = topk_value((uint32_t)(pair >> 32));
+            idx[(size_t)n * t + p] = topk_class(pair);
+        }
+    });
+    if (parts > 1)
+        for (int i = all + threadIdx.x; i < t; i += TH) pairs[((size_t)n * parts + s) * t + i] = 0;
+}
+
+// The t largest of a row's sorted lists.  The bound is again the smallest of the lists' r-th entries, r = t / lists; the pairs that reach
+// it are few, or else each finds its place by bisection in every list.
+constexpr int kTopkMergeThreads = 512, kTopkMergeMost = 6144;  // pairs of a row
+__global__ __launch_bounds__(kTopkMergeThreads) void topk_merge_kernel(int t, int parts, const uint64_t *__restrict__ pairs, float *__restrict__ val,
+                                                                       int32_t *__restrict__ idx)
+{
+    __shared__ uint64_t list[kTopkMergeMost], found[kTopkFound];
+    __shared__ int place[kTopkFound], total;
+    const int n = blockIdx.x, all = parts * t, lane = threadIdx.x & 63;
+    for (int i = threadIdx.x; i < all; i += kTopkMergeThreads) list[i] = pairs[(size_t)n * all + i];
+    for (int i = threadIdx.x; i < kTopkFound; i += kTopkMergeThreads) place[i] = 0;
+    if (threadIdx.x == 0) total = 0;
+    __syncthreads();
+    const int r = (t + parts - 1) / parts;
+    uint64_t L = ~0ull;
+    for (int p = lane; p < parts; p += 64) L = min(L, list[p * t + r - 1]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) L = min(L, (uint64_t)__shfl_xor((unsigned long long)L, o, 64));
+    if (L == 0) L = 1;  // a zero is no element
+    for (int i = threadIdx.x; i < all; i += kTopkMergeThreads)
+        if (list[i] >= L) {
+            const int slot = atomicAdd(&total, 1);
+            if (slot < kTopkFound) found[slot] = list[i];
+        }
+    __syncthreads();
+    auto put = [&](int p, uint64_t pair) {
+        val[(size_t)n * t + p] = topk_value((uint32_t)(pair >> 32));
+        idx[(size_t)n * t + p] = topk_class(pair);
+    };
+    if (total <= kTopkFound) return topk_places<kTopkMergeThreads>(t, total, found, place, put);
+    for (int i = threadIdx.x; i < all; i += kTopkMergeThreads) {
+        const uint64_t own = list[i];
+        if (own < L) continue;
+        int larger = 0;
+        for (int p = 0; p < parts && larger < t; ++p) {
+            int lo = 0, hi = t;
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (list[p * t + mid] > own) lo = mid + 1;
+                else hi = mid;
+            }
+            larger += lo;
+        }
+        if (larger < t) put(larger, own);
+    }
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------------
+// Parts of a row: as many as its length wants (a workgroup keeps 32768 elements), more where the rows are too few for the chip, of at
+// least 4096 elements.
+struct TopkCut { int parts, per; };
+static TopkCut topk_cut(int n, int k, int t)
+{
+    constexpr int kMost = 32768, kLeast = 4096, kWorkgroups = 512;
+    long parts = ceil_div(k, kMost);
+    const long wanted = kWorkgroups / n, most = ceil_div(k, kLeast);
+    if (parts < wanted) parts = wanted < most ? wanted : most;
+    const int lists = kTopkMergeMost / t < 64 ? kTopkMergeMost / t : 64;  // what the merge holds
+    if (parts > lists && ceil_div(k, lists) <= kMost) parts = lists;
+    if (parts < 1) parts = 1;
+    const int per = (int)((ceil_div(k, parts) + 7) & ~7L);
+    return {ceil_div(k, per), per};
+}
+
+template <class T>
+static int topk_impl(const char *who, int n, int k, int t, const T *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes,
+                     void *stream)
+{
+    RN50_REQUIRE(n > 0 && k > 0 && t > 0, RN50_EINVAL, "%s: non-positive dimension", who);
+    RN50_REQUIRE(n < kMaxRows, RN50_EUNSUPPORTED, "%s: 2^22 rows and more", who);
+    RN50_REQUIRE(t <= k, RN50_EINVAL, "%s: more logits asked for than a row has", who);
+    RN50_REQUIRE(t <= RN50_TOPK_MAX, RN50_EUNSUPPORTED, "%s: at most %d logits of a row", who, RN50_TOPK_MAX);
+    RN50_REQUIRE(ld >= (size_t)k && ld < (1ull << 31), RN50_EINVAL, "%s: rows overlap or are 2^31 elements apart and more", who);
+    RN50_REQUIRE(logits && val && idx, RN50_EINVAL, "%s: null pointer", who);
+    RN50_REQUIRE(aligned16(logits) && aligned16(val) && aligned16(idx) && aligned16(ws), RN50_EINVAL, "%s: pointers must be 16-byte aligned", who);
+    const TopkCut cut = topk_cut(n, k, t);
+    RN50_REQUIRE(cut.parts * (long)t <= kTopkMergeMost, RN50_EUNSUPPORTED, "%s: %d logits of rows of %d", who, t, k);
+    RN50_REQUIRE(cut.parts == 1 || ws, RN50_EINVAL, "%s: null pointer", who);
+    RN50_REQUIRE(cut.parts == 1 || ws_bytes >= sizeof(uint64_t) * n * cut.parts * t, RN50_EWORKSPACE, "%s: workspace too small", who);
+    uint64_t *pairs = (uint64_t *)ws;
+    hipStream_t st = (hipStream_t)stream;
+    constexpr int VEC = RowVec<T>::N;
+    const dim3 grid((unsigned)((long)n * cut.parts));
+    // one vector to a thread in short rows, then four, then 512 threads (whose eight bounds suit t = 256) with all that is left
+    if (cut.per <= 64 * VEC) hipLaunchKernelGGL((topk_kernel<T, 64, 1>), grid, dim3(64), 0, st, k, t, cut.parts, cut.per, logits, ld, val, idx, pairs);
+    else if (cut.per <= 256 * VEC) hipLaunchKernelGGL((topk_kernel<T, 256, 1>), grid, dim3(256), 0, st, k, t, cut.parts, cut.per, logits, ld, val, idx, pairs);
+    else if (cut.per <= 1024 * VEC) hipLaunchKernelGGL((topk_kernel<T, 256, 4>), grid, dim3(256), 0, st, k, t, cut.parts, cut.per, logits, ld, val, idx, pairs);
+    else hipLaunchKernelGGL((topk_kernel<T, 512, 64 / VEC>), grid, dim3(512), 0, st, k, t, cut.parts, cut.per, logits, ld, val, idx, pairs);
+    if (cut.parts > 1) hipLaunchKernelGGL(topk_merge_kernel, dim3(n), dim3(kTopkMergeThreads), 0, st, t, cut.parts, pairs, val, idx);
+    return launch_status(who);
+}
+
+}  // namespace rn50
+
+using namespace rn50;
+
+extern "C" size_t rn50_topk_workspace_bytes(int n, int k, int t)
+{
+    if (n <= 0 || n >= kMaxRows || k <= 0 || t <= 0 || t > k || t > RN50_TOPK_MAX) return 0;
+    const TopkCut cut = topk_cut(n, k, t);
+    return cut.parts == 1 || cut.parts * (long)t > kTopkMergeMost ? 0 : sizeof(uint64_t) * n * cut.parts * t;
+}
+
+extern "C" int logits_topk(int n, int k, int t, const float *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes, void *stream)
+{
+    return topk_impl<float>("logits_topk", n, k, t, logits, ld, val, idx, ws, ws_bytes, stream);
+}
+extern "C" int logits_topk_bf16(int n, int k, int t, const uint16_t *logits, size_t ld, float *val, int32_t *idx, void *ws, size_t ws_bytes,
+                                void *stream)
+{
+    return topk_impl<bf16_t>("logits_topk_bf16", n, k, t, logits, ld, val, idx, ws, ws_bytes, stream);
+}
