@@ -415,7 +415,7 @@ int softmax_ce(int n, int k, const float *logits, const int32_t *labels, float *
  * Learning from a teacher (Hinton et al. 2015) of which only the largest logits of each row are kept.
  * logits: N rows of K classes, row n starting at logits + n*ld elements (ld >= K: a row may be padded; what lies behind
  * its K classes is neither read nor written).  The _bf16 calls take logits (and write their gradient) as bfloat16 bits;
- * everything else is fp32.  Rows of any length, fewer than 2^22 of them;
+ * everything else is fp32.  Rows of any length, fewer than 2^22 of them (or of the parts that long ones are cut into);
  * t in [1, RN50_TOPK_MAX].
  * ------------------------------------------------------------------------------------------ */
 #define RN50_TOPK_MAX 256
@@ -440,9 +440,9 @@ int logits_topk_bf16(int n, int k, int t, const uint16_t *logits, size_t ld, flo
  * teacher_val NULL; loss[2] is 0).  tau in [1/1024, 1024].
  * labels: N int32; teacher_idx, teacher_val: N x t, rows one behind the other (logits_topk's output).  An index of -1 or a
  * kept logit of -infinity keeps nothing; a class that occurs twice in a row counts twice.  Any other label or index outside
- * [0, K) is no error code (they are device memory): it makes the loss NaN and contributes no term to the gradient.  A class
- * masked by -infinity or the type's lowest value has q = r = 0 and no gradient of its own; where the label or a kept class is
- * masked by -infinity, the loss is infinite and the gradient finite.  A row of nothing but -infinity, or with a NaN or
+ * [0, K) is no error code (they are device memory): it makes the loss NaN, and its one-hot term or its p_t is left out of the
+ * gradient.  A class masked by -infinity or the type's lowest value has q = r = 0 and no gradient of its own; where the label
+ * or a kept class is masked by -infinity, the loss is infinite and the gradient finite.  A row of nothing but -infinity, or with a NaN or
  * +infinity, has NaN for its gradient and makes the loss NaN.  A row that has no label and keeps nothing counts for nothing,
  * whatever its logits: its gradient is 0.
  * loss: 3 floats.  dlogits: row n at dlogits + n*ld_dlogits (ld_dlogits >= K), not in place; NULL: the loss alone.

@@ -1,25 +1,15 @@
 // Learning from a teacher's largest logits (Hinton et al. 2015): the cross-entropy with the label and with them, with its gradient.
+//
+// A row is read once: its workgroup keeps it in registers, takes the maximum, the sums of exp(z - max) and exp((z - max)/tau), and goes
+// over the registers again for the gradient.  Exponentials are formed twice (kept, they would take the registers that let several rows
+// share a compute unit): up to four for an element, which cost about what its four bytes of memory traffic (bf16) do.  The label's and the
+// kept classes' elements are written again with their own terms once the row is out.  Rows too long for that, and few long rows, are
+// cut into parts: one launch for the parts' maxima and sums, one for the loss and the gradient.
+#include <type_traits>
+
 #include "rows.h"
 
 namespace rn50 {
-
-constexpr int kRowThreads = 256;
-
-template <class Op>
-__device__ inline float row_reduce(float v, float *red, Op op)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-    for (int w = 1; w < kRowThreads / 64; ++w) v = op(v, red[w]);
-    return v;
-}
-struct Sum { __device__ float operator()(float a, float b) const { return a + b; } };
-// a NaN stays one
-struct Max { __device__ float operator()(float a, float b) const { return a > b || a != a ? a : b; } };
 
 struct DistillArgs {
     int K, t;
@@ -28,108 +18,277 @@ struct DistillArgs {
     const int32_t *idx;     // null: no soft term
     const float *val;
     float alpha, tau, scale;
+    float c1, ct;           // log2(e), log2(e)/tau
+    int parts, per;         // workgroups to a row, elements of each (a multiple of the vector)
 };
+constexpr float kLn2 = 0.693147181f;
 
-template <class T>
-__global__ __launch_bounds__(kRowThreads) void distill_kernel(DistillArgs a, const T *__restrict__ z, T *__restrict__ dz, float *__restrict__ row_loss)
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }  // one rounding or so; 0 below 2^-126
+
+template <class T, int N> __device__ inline void row_unpack(const uint4 &v, float (&f)[N])
 {
-    __shared__ float red[kRowThreads / 64], p[RN50_TOPK_MAX];
-    __shared__ int at[RN50_TOPK_MAX];
-    const int K = a.K, tid = threadIdx.x, n = blockIdx.x;
-    const T *row = z + n * a.ld;
-    T *out = dz + n * a.ld_d;
-    const float nan = __builtin_nanf("");
-    // the teacher's entry tid (t <= kRowThreads)
-    int k = -1;
-    float v = -INFINITY;
-    if (a.idx && tid < a.t) {
-        k = a.idx[(size_t)n * a.t + tid];
-        v = k != -1 ? a.val[(size_t)n * a.t + tid] : -INFINITY;
-    }
-    const bool kept = v > -INFINITY || v != v, class_ok = (unsigned)k < (unsigned)K;
-    const float vmx = row_reduce(v, red, Max());
-    const bool some = vmx > -INFINITY || vmx != vmx;
-    const int label = a.labels ? a.labels[n] : -1;
-    const bool has = label != -1, label_ok = (unsigned)label < (unsigned)K;
-    if (!has && !some) {  // a row that counts for nothing, whatever its logits
-        if (tid == 0) row_loss[2 * n] = row_loss[2 * n + 1] = 0.f;
-        if (dz)
-            for (int c = tid; c < K; c += kRowThreads) row_st(out, c, 0.f);
-        return;
-    }
-    float mx = -INFINITY;
-    for (int k = tid; k < K; k += kRowThreads) mx = Max()(mx, row_ld(row, k));
-    mx = row_reduce(mx, red, Max());
-    float s1 = 0.f, st = 0.f;
-    for (int k = tid; k < K; k += kRowThreads) {
-        const float d = row_ld(row, k) - mx;
-        s1 += expf(d);
-        st += expf(d / a.tau);
-    }
-    s1 = row_reduce(s1, red, Sum());
-    st = row_reduce(st, red, Sum());
-
-    float hard = 0.f, soft = 0.f;
-    bool bad = false;
-    if (has) {
-        if (label_ok) hard = logf(s1) - (row_ld(row, label) - mx);
-        else bad = true;
-    }
-    const float d = (v - vmx) / a.tau, e = kept ? expf(d) : 0.f;
-    const float se = row_reduce(e, red, Sum());
-    const float pt = kept ? e / se : 0.f;
-    float term = 0.f;
-    if (kept && class_ok && pt != 0.f) term = pt * ((d - logf(se)) - ((row_ld(row, k) - mx) / a.tau - logf(st)));
-    if (kept && !class_ok) term = nan;
-    if (some) soft = a.tau * a.tau * row_reduce(term, red, Sum());
-    if (tid == 0) {
-        row_loss[2 * n] = bad || s1 != s1 ? nan : hard;
-        row_loss[2 * n + 1] = s1 != s1 ? nan : soft;
-    }
-    if (!dz) return;
-    __syncthreads();
-    p[tid] = pt;
-    at[tid] = kept && class_ok ? k : -1;
-    __syncthreads();
-    const float w1 = has ? (1.f - a.alpha) * a.scale : 0.f, wt = some ? a.alpha * a.tau * a.scale : 0.f;
-    auto grad = [&](int c) {
-        const float x = row_ld(row, c) - mx;
-        float g = 0.f;
-        if (has) g += w1 * (expf(x) / s1 - (c == label ? 1.f : 0.f));
-        if (some) g += wt * (expf(x / a.tau) / st);
-        return s1 != s1 ? nan : g;
-    };
-    for (int c = tid; c < K; c += kRowThreads) row_st(out, c, grad(c));
-    __syncthreads();
-    // the teacher's classes again, less their probabilities; the first entry of a class writes for all of it
-    if (at[tid] >= 0 && tid < a.t) {
-        float sum = 0.f;
-        bool first = true;
-        for (int i = 0; i < a.t; ++i)
-            if (at[i] == at[tid]) {
-                first = first && i >= tid;
-                sum += p[i];
-            }
-        if (first) row_st(out, at[tid], grad(at[tid]) - wt * sum);
+    if constexpr (N == 4) {
+        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+    } else {
+        f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+        f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
     }
 }
-
-// loss[0..2] from the rows' terms; each thread adds every 256th row, in 64 bits
-__global__ __launch_bounds__(kRowThreads) void distill_loss_kernel(int N, float alpha, float scale, const float *__restrict__ row_loss,
-                                                                   float *__restrict__ loss)
+template <class T, int N> __device__ inline uint4 row_pack(const float (&f)[N])
 {
-    __shared__ double part[2][kRowThreads];
-    double h = 0., s = 0.;
-    for (int n = threadIdx.x; n < N; n += kRowThreads) {
-        h += row_loss[2 * (size_t)n];
-        s += row_loss[2 * (size_t)n + 1];
+    if constexpr (N == 4) return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    else return make_uint4(bf16_pack2(f[0], f[1]), bf16_pack2(f[2], f[3]), bf16_pack2(f[4], f[5]), bf16_pack2(f[6], f[7]));
+}
+// Sum of a vector's values, in pairs.
+template <int N> __device__ inline float tree_sum(const float (&f)[N])
+{
+    const float s = (f[0] + f[1]) + (f[2] + f[3]);
+    if constexpr (N == 8) return s + ((f[4] + f[5]) + (f[6] + f[7]));
+    return s;
+}
+
+// K values over the workgroup, in every thread; buf: K * WAVES floats that no other call uses.
+template <int K, int WAVES, class Op> __device__ inline void block_reduce(float (&v)[K], float *buf, Op op)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = op(v[k], __shfl_xor(v[k], o, 64));
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) buf[k * WAVES + (threadIdx.x >> 6)] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float w[WAVES];
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) w[i] = buf[k * WAVES + i];
+#pragma unroll
+        for (int half = WAVES / 2; half; half /= 2)
+#pragma unroll
+            for (int i = 0; i < half; ++i) w[i] = op(w[i], w[i + half]);
+        v[k] = w[0];
     }
-    part[0][threadIdx.x] = h;
-    part[1][threadIdx.x] = s;
+}
+struct Sum { __device__ float operator()(float a, float b) const { return a + b; } };
+struct Max { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };  // of a NaN and a number the number; the sums keep the NaN
+
+// A part of a row in the registers of a workgroup: whole vectors, and the elements behind them, one to a thread.
+template <class T, int TH, int E> struct RowPart {
+    static constexpr int VEC = RowVec<T>::N;
+    uint4 raw[E];
+    float rest;
+    int len, whole;
+    __device__ void load(const T *row, int length)
+    {
+        len = length;
+        whole = len - len % VEC;
+        const uint32_t lowest = VEC == 4 ? 0xff800000u : 0xff80ff80u;  // -infinity adds nothing
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int at = (e * TH + (int)threadIdx.x) * VEC;
+            raw[e] = make_uint4(lowest, lowest, lowest, lowest);
+            if (at < whole) raw[e] = row_load16(row + at);
+        }
+        rest = whole + (int)threadIdx.x < len ? row_ld(row, whole + threadIdx.x) : -INFINITY;
+    }
+    __device__ float largest() const
+    {
+        float m = rest;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e * TH * VEC < whole) {
+                float f[VEC];
+                row_unpack<T, VEC>(raw[e], f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) m = fmaxf(m, f[i]);
+            }
+        return m;
+    }
+    // this thread's sums of 2^((z - mx)*a) and, if two, of 2^((z - mx)*b)
+    __device__ void sums(float mx, float a, float b, bool two, float &sa, float &sb) const
+    {
+        sa = sb = 0.f;
+        if (whole + (int)threadIdx.x < len) {
+            sa = exp2_fast((rest - mx) * a);
+            if (two) sb = exp2_fast((rest - mx) * b);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e * TH * VEC < whole && (e * TH + (int)threadIdx.x) * VEC < whole) {
+                float f[VEC], g[VEC];
+                row_unpack<T, VEC>(raw[e], f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    f[i] -= mx;
+                    g[i] = exp2_fast(f[i] * a);
+                }
+                sa += tree_sum<VEC>(g);
+                if (two) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) g[i] = exp2_fast(f[i] * b);
+                    sb += tree_sum<VEC>(g);
+                }
+            }
+    }
+};
+
+// The maximum of a part and its sums at both temperatures: stats[row][part] = {max, sum, sum at tau}.  A part of nothing but -infinity sums
+// to 0.
+template <class T, int TH, int E>
+__global__ __launch_bounds__(TH) void distill_stats_kernel(DistillArgs a, const T *__restrict__ z, float4 *__restrict__ stats)
+{
+    constexpr int WAVES = TH / 64;
+    __shared__ float buf[3 * WAVES];
+    const int n = blockIdx.x / a.parts, s = blockIdx.x % a.parts, first = s * a.per;
+    RowPart<T, TH, E> part;
+    part.load(z + n * a.ld + first, min(a.per, a.K - first));
+    float m[1] = {part.largest()};
+    block_reduce<1, WAVES>(m, buf, Max());
+    const float mx = m[0] == -INFINITY ? 0.f : m[0];
+    const bool hard = a.labels != nullptr, two = hard && a.idx && a.tau != 1.f;
+    float v[2];
+    part.sums(mx, hard ? a.c1 : a.ct, a.ct, two, v[0], v[1]);
+    block_reduce<2, WAVES>(v, buf + WAVES, Sum());
+    if (threadIdx.x == 0) stats[blockIdx.x] = make_float4(m[0], v[0], two ? v[1] : v[0], 0.f);
+}
+
+// Row n's loss terms, and the gradient of its part; SPLIT: from the parts' statistics, otherwise the row has one part.
+template <class T, int TH, int E, bool SPLIT>
+__global__ __launch_bounds__(TH) void distill_kernel(DistillArgs a, int grad_parts, const T *__restrict__ z, const float4 *__restrict__ stats,
+                                                     T *__restrict__ dz, float *__restrict__ row_loss)
+{
+    constexpr int WAVES = TH / 64, VEC = RowVec<T>::N;
+    __shared__ float buf[7 * WAVES], p_at[RN50_TOPK_MAX];
+    __shared__ int class_at[RN50_TOPK_MAX], label_kept;
+    const int n = blockIdx.x / grad_parts, s = blockIdx.x % grad_parts, first = s * a.per, tid = threadIdx.x, K = a.K;
+    const T *row = z + n * a.ld;
+    const float nan = __builtin_nanf("");
+    RowPart<T, TH, E> part;
+    if (!SPLIT || dz) part.load(row + first, min(a.per, K - first));
+    const int label = a.labels ? a.labels[n] : -1;
+    const bool has = label != -1, label_ok = (unsigned)label < (unsigned)K;
+    int k = -1;
+    float v = -INFINITY;
+    if (a.idx && tid < a.t) {  // the teacher's entry tid
+        k = a.idx[(size_t)n * a.t + tid];
+        v = a.val[(size_t)n * a.t + tid];
+    }
+    const bool kept = k != -1 && v != -INFINITY, class_ok = kept && (unsigned)k < (unsigned)K;
+    const float z_kept = class_ok ? row_ld(row, k) : 0.f, z_label = has && label_ok ? row_ld(row, label) : 0.f;
+
+    float m[2] = {kept ? (v == v ? v : INFINITY) : -INFINITY, SPLIT ? -INFINITY : part.largest()};
+    if (SPLIT) {  // every wavefront: the parts' maxima
+        for (int q = tid & 63; q < a.parts; q += 64) m[1] = fmaxf(m[1], stats[(size_t)n * a.parts + q].x);
+    }
+    if (tid == 0) label_kept = 0;
+    block_reduce<2, WAVES>(m, buf, Max());
+    const bool some = m[0] > -INFINITY;
+    const float mx = m[1];
+    T *out = dz + n * a.ld_d + first;
+    const int len = min(a.per, K - first), whole = len - len % VEC;
+    if (!has && !some) {  // a row that counts for nothing, whatever its logits
+        if (s == 0 && tid == 0) row_loss[2 * n] = row_loss[2 * n + 1] = 0.f;
+        if (!dz) return;
+        for (int at = tid * VEC; at < whole; at += TH * VEC) row_store16(out + at, make_uint4(0, 0, 0, 0));
+        if (whole + tid < len) row_st(out, whole + tid, 0.f);
+        return;
+    }
+    const bool two = has && some && a.tau != 1.f;  // two softmaxes
+    const float ca = has ? a.c1 : a.ct;
+    float q[3] = {kept ? exp2_fast((v - m[0]) * a.ct) : 0.f, 0.f, 0.f};
+    if (SPLIT) {
+        if (tid < 64)
+            for (int i = tid; i < a.parts; i += 64) {
+                const float4 st = stats[(size_t)n * a.parts + i];
+                q[1] = fmaf(has ? st.y : st.z, exp2_fast((st.x - mx) * ca), q[1]);
+                q[2] = fmaf(st.z, exp2_fast((st.x - mx) * a.ct), q[2]);
+            }
+    } else {
+        part.sums(mx, ca, a.ct, two, q[1], q[2]);
+    }
+    block_reduce<3, WAVES>(q, buf + 2 * WAVES, Sum());
+    const float sa = q[1], st = two ? q[2] : sa, pt = kept ? q[0] == q[0] ? exp2_fast((v - m[0]) * a.ct) / q[0] : nan : 0.f;
+    float l[2] = {0.f, 0.f};
+    if (kept && !class_ok) l[0] = nan;
+    else if (kept && pt != 0.f)
+        l[0] = pt * (((v - m[0]) * a.ct - (z_kept - mx) * a.ct) * kLn2 - (logf(q[0]) - logf(st)));
+    if (class_ok && k == label) label_kept = 1;
+    if (tid < a.t) {
+        p_at[tid] = pt;
+        class_at[tid] = class_ok ? k : -1;
+    }
+    block_reduce<2, WAVES>(l, buf + 5 * WAVES, Sum());
+    if (s == 0 && tid == 0) {
+        row_loss[2 * n] = !has ? 0.f : label_ok ? logf(sa) - (z_label - mx) : nan;
+        row_loss[2 * n + 1] = some ? a.tau * a.tau * l[0] : 0.f;
+        if (sa != sa) row_loss[2 * n] = row_loss[2 * n + 1] = nan;
+    }
+    if (!dz) return;
+
+    // dz = e_a*ka + e_b*kb, the softmaxes with their weights
+    const float w1 = has ? (1.f - a.alpha) * a.scale : 0.f, wt = some ? a.alpha * a.tau * a.scale : 0.f;
+    const float kb = two ? wt / st : 0.f, ka = two ? w1 / sa : (w1 + wt) / sa, cb = a.ct;
+    auto grad = [&](float x) {
+        const float d = x - mx, g = exp2_fast(d * ca) * ka;
+        return two ? fmaf(exp2_fast(d * cb), kb, g) : g;
+    };
+    // a kept class in this part: the first entry of it writes for all of them
+    float kept_sum = 0.f;
+    bool writes = class_ok && (unsigned)(k - first) < (unsigned)len;
+    if (__ballot(writes))
+        for (int i = 0; i < a.t; ++i)
+            if (class_at[i] == k) {
+                writes = writes && i >= tid;
+                kept_sum += p_at[i];
+            }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int at = (e * TH + tid) * VEC;
+        if (at < whole) {
+            float f[VEC], g[VEC];
+            row_unpack<T, VEC>(part.raw[e], f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                f[i] -= mx;
+                g[i] = exp2_fast(f[i] * ca) * ka;
+            }
+            if (two)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) g[i] = fmaf(exp2_fast(f[i] * cb), kb, g[i]);
+            row_store16(out + at, row_pack<T, VEC>(g));
+        }
+    }
+    if (whole + tid < len) row_st(out, whole + tid, grad(part.rest));
+    __syncthreads();  // the classes below are written a second time
+    if (writes) row_st(out, k - first, grad(z_kept) - fmaf(wt, kept_sum, k == label ? w1 : 0.f));
+    if (tid == TH - 1 && has && label_ok && !label_kept && (unsigned)(label - first) < (unsigned)len) row_st(out, label - first, grad(z_label) - w1);
+}
+
+// loss[0..2] from the rows' terms, in 64 bits
+constexpr int kLossThreads = 1024;
+__global__ __launch_bounds__(kLossThreads) void distill_loss_kernel(int N, float alpha, float scale, const float *__restrict__ row_loss,
+                                                                    float *__restrict__ loss)
+{
+    __shared__ double part[2][kLossThreads / 64];
+    double h = 0., s = 0.;
+    for (int n = threadIdx.x; n < N; n += kLossThreads) {
+        const float2 v = reinterpret_cast<const float2 *>(row_loss)[n];
+        h += v.x;
+        s += v.y;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        h += __shfl_xor(h, o, 64);
+        s += __shfl_xor(s, o, 64);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        part[0][threadIdx.x >> 6] = h;
+        part[1][threadIdx.x >> 6] = s;
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
-        h = s = 0.;
-        for (int i = 0; i < kRowThreads; ++i) {
+        for (int i = 1; i < kLossThreads / 64; ++i) {
             h += part[0][i];
             s += part[1][i];
         }
@@ -142,7 +301,31 @@ __global__ __launch_bounds__(kRowThreads) void distill_loss_kernel(int N, float 
     }
 }
 
-static size_t distill_ws_bytes(int n) { return (size_t)2 * n * sizeof(float); }
+// ---- host side -------------------------------------------------------------------------------------------------------------
+// One part where a workgroup of 1024 threads holds the row (in vectors of 16 bytes, eight to a thread) and the rows fill the chip; few
+// long rows in parts of 4096 elements or more.
+struct DistillCut { int parts, per; };
+static DistillCut distill_cut(int n, int k, int vec)
+{
+    constexpr int kLeast = 4096, kWorkgroups = 512;
+    long parts = ceil_div(k, 1024L * 8 * vec);
+    const long wanted = kWorkgroups / n, most = ceil_div(k, kLeast);
+    if (parts < wanted) parts = wanted < most ? wanted : most;
+    if (parts < 1) parts = 1;
+    const int per = (int)((ceil_div(k, parts) + 7) & ~7L);
+    return {ceil_div(k, per), per};
+}
+// Rows' loss terms, parts' statistics (enough for either type).
+static size_t distill_loss_floats(int n) { return ((size_t)2 * n + 3) & ~(size_t)3; }
+static size_t distill_ws_bytes(int n, int k)
+{
+    size_t parts = 0;
+    for (int vec : {4, 8}) {
+        const DistillCut cut = distill_cut(n, k, vec);
+        if (cut.parts > 1 && (size_t)cut.parts > parts) parts = cut.parts;
+    }
+    return (distill_loss_floats(n) + parts * 4 * (size_t)n) * sizeof(float);
+}
 
 template <class T>
 static int distill_impl(const char *who, int n, int k, int t, const T *logits, size_t ld, const int32_t *labels, const int32_t *teacher_idx,
@@ -166,11 +349,33 @@ static int distill_impl(const char *who, int n, int k, int t, const T *logits, s
                      aligned16(dlogits) && aligned16(ws),
                  RN50_EINVAL, "%s: pointers must be 16-byte aligned", who);
     RN50_REQUIRE(dlogits != logits, RN50_EINVAL, "%s: not in place", who);
-    RN50_REQUIRE(ws_bytes >= distill_ws_bytes(n), RN50_EWORKSPACE, "%s: workspace too small", who);
-    const DistillArgs a{k, t, ld, dlogits ? ld_d : 0, alpha < 1.f ? labels : nullptr, alpha > 0.f ? teacher_idx : nullptr, teacher_val, alpha, tau, scale};
+    RN50_REQUIRE(ws_bytes >= distill_ws_bytes(n, k), RN50_EWORKSPACE, "%s: workspace too small", who);
+    constexpr int VEC = RowVec<T>::N;
+    const DistillCut cut = distill_cut(n, k, VEC);
+    RN50_REQUIRE((long)n * cut.parts < kMaxRows, RN50_EUNSUPPORTED, "%s: too many long rows", who);
+    const double log2e = 1.4426950408889634;
+    const DistillArgs a{k, t, ld, dlogits ? ld_d : 0, alpha < 1.f ? labels : nullptr, alpha > 0.f ? teacher_idx : nullptr, teacher_val, alpha, tau, scale,
+                        (float)log2e, (float)(log2e / tau), cut.parts, cut.per};
     float *row_loss = (float *)ws;
-    hipLaunchKernelGGL((distill_kernel<T>), dim3(n), dim3(kRowThreads), 0, (hipStream_t)stream, a, logits, dlogits, row_loss);
-    hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kRowThreads), 0, (hipStream_t)stream, n, alpha, scale, row_loss, loss);
+    float4 *stats = reinterpret_cast<float4 *>(row_loss + distill_loss_floats(n));
+    hipStream_t st = (hipStream_t)stream;
+    auto launch = [&](auto threads, auto vectors) {
+        constexpr int TH = decltype(threads)::value, E = decltype(vectors)::value;
+        if (cut.parts == 1) {
+            hipLaunchKernelGGL((distill_kernel<T, TH, E, false>), dim3(n), dim3(TH), 0, st, a, 1, logits, nullptr, dlogits, row_loss);
+        } else {
+            hipLaunchKernelGGL((distill_stats_kernel<T, TH, E>), dim3((unsigned)((long)n * cut.parts)), dim3(TH), 0, st, a, logits, stats);
+            const int grad_parts = dlogits ? cut.parts : 1;
+            hipLaunchKernelGGL((distill_kernel<T, TH, E, true>), dim3((unsigned)((long)n * grad_parts)), dim3(TH), 0, st, a, grad_parts, logits, stats, dlogits,
+                               row_loss);
+        }
+    };
+    using std::integral_constant;
+    if (cut.per <= 256 * VEC) launch(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    else if (cut.per <= 1024 * VEC) launch(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else if (cut.per <= 4096 * VEC) launch(integral_constant<int, 512>{}, integral_constant<int, 8>{});
+    else launch(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+    hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kLossThreads), 0, st, n, alpha, scale, row_loss, loss);
     return launch_status(who);
 }
 
@@ -180,7 +385,7 @@ using namespace rn50;
 
 extern "C" size_t rn50_distill_workspace_bytes(int n, int k, int t)
 {
-    return n > 0 && k > 0 && t >= 0 ? distill_ws_bytes(n) : 0;
+    return n > 0 && k > 0 && t >= 0 ? distill_ws_bytes(n, k) : 0;
 }
 
 extern "C" int distill_ce(int n, int k, int t, const float *logits, size_t ld, const int32_t *labels_or_null, const int32_t *teacher_idx,

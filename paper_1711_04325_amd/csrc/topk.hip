@@ -345,6 +345,7 @@ static int topk_impl(const char *who, int n, int k, int t, const T *logits, size
     RN50_REQUIRE(aligned16(logits) && aligned16(val) && aligned16(idx) && aligned16(ws), RN50_EINVAL, "%s: pointers must be 16-byte aligned", who);
     const TopkCut cut = topk_cut(n, k, t);
     RN50_REQUIRE(cut.parts * (long)t <= kTopkMergeMost, RN50_EUNSUPPORTED, "%s: %d logits of rows of %d", who, t, k);
+    RN50_REQUIRE((long)n * cut.parts < kMaxRows, RN50_EUNSUPPORTED, "%s: too many long rows", who);
     RN50_REQUIRE(cut.parts == 1 || ws, RN50_EINVAL, "%s: null pointer", who);
     RN50_REQUIRE(cut.parts == 1 || ws_bytes >= sizeof(uint64_t) * n * cut.parts * t, RN50_EWORKSPACE, "%s: workspace too small", who);
     uint64_t *pairs = (uint64_t *)ws;
