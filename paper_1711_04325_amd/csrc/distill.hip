@@ -47,6 +47,25 @@ template <int N> __device__ inline float tree_sum(const float (&f)[N])
     return s;
 }
 
+// The softmax at temperature 1 beside that at tau: exp(d) is exp(d/tau) to the power of tau, one or two multiplications for temperatures
+// of 2 and 4 (whose roundings, tau times that of the root, are as many as an exponential's of d) in place of an exponential, which costs
+// four.  4096 x 32768 bf16 at tau = 2: 124 us -> 119.
+template <int N> __device__ inline void two_exps(const float (&d)[N], float a, float b, float tau, float (&ea)[N], float (&eb)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) eb[i] = exp2_fast(d[i] * b);
+    if (tau == 2.f || tau == 4.f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) ea[i] = eb[i] * eb[i];
+        if (tau == 4.f)
+#pragma unroll
+            for (int i = 0; i < N; ++i) ea[i] *= ea[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) ea[i] = exp2_fast(d[i] * a);
+    }
+}
+
 // K values over the workgroup, in every thread; buf: K * WAVES floats that no other call uses.
 template <int K, int WAVES, class Op> __device__ inline void block_reduce(float (&v)[K], float *buf, Op op)
 {
@@ -105,8 +124,8 @@ template <class T, int TH, int E> struct RowPart {
             }
         return m;
     }
-    // this thread's sums of 2^((z - mx)*a) and, if two, of 2^((z - mx)*b)
-    __device__ void sums(float mx, float a, float b, bool two, float &sa, float &sb) const
+    // this thread's sums of 2^((z - mx)*a) and, if two, of 2^((z - mx)*b), b = a/tau
+    __device__ void sums(float mx, float a, float b, float tau, bool two, float &sa, float &sb) const
     {
         sa = sb = 0.f;
         if (whole + (int)threadIdx.x < len) {
@@ -116,19 +135,18 @@ template <class T, int TH, int E> struct RowPart {
 #pragma unroll
         for (int e = 0; e < E; ++e)
             if (e * TH * VEC < whole && (e * TH + (int)threadIdx.x) * VEC < whole) {
-                float f[VEC], g[VEC];
+                float f[VEC], g[VEC], h[VEC];
                 row_unpack<T, VEC>(raw[e], f);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    f[i] -= mx;
-                    g[i] = exp2_fast(f[i] * a);
+                for (int i = 0; i < VEC; ++i) f[i] -= mx;
+                if (two) {
+                    two_exps<VEC>(f, a, b, tau, g, h);
+                    sb += tree_sum<VEC>(h);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) g[i] = exp2_fast(f[i] * a);
                 }
                 sa += tree_sum<VEC>(g);
-                if (two) {
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) g[i] = exp2_fast(f[i] * b);
-                    sb += tree_sum<VEC>(g);
-                }
             }
     }
 };
@@ -148,19 +166,22 @@ __global__ __launch_bounds__(TH) void distill_stats_kernel(DistillArgs a, const 
     const float mx = m[0] == -INFINITY ? 0.f : m[0];
     const bool hard = a.labels != nullptr, two = hard && a.idx && a.tau != 1.f;
     float v[2];
-    part.sums(mx, hard ? a.c1 : a.ct, a.ct, two, v[0], v[1]);
+    part.sums(mx, hard ? a.c1 : a.ct, a.ct, a.tau, two, v[0], v[1]);
     block_reduce<2, WAVES>(v, buf + WAVES, Sum());
     if (threadIdx.x == 0) stats[blockIdx.x] = make_float4(m[0], v[0], two ? v[1] : v[0], 0.f);
 }
 
+// (Registers: room for three workgroups of 512 threads, 4096 x 32768 bf16 in 131 us; left to itself the compiler takes some more, and two
+// fit: 145.  Four fit with spills: 156.  Workgroups of 1024 threads, of which one fits: 222.)
 // Row n's loss terms, and the gradient of its part; SPLIT: from the parts' statistics, otherwise the row has one part.
 template <class T, int TH, int E, bool SPLIT>
-__global__ __launch_bounds__(TH) void distill_kernel(DistillArgs a, int grad_parts, const T *__restrict__ z, const float4 *__restrict__ stats,
+__global__ __launch_bounds__(TH, E > 8 ? 4 : 6) void distill_kernel(DistillArgs a, int grad_parts, const T *__restrict__ z, const float4 *__restrict__ stats,
                                                      T *__restrict__ dz, float *__restrict__ row_loss)
 {
     constexpr int WAVES = TH / 64, VEC = RowVec<T>::N;
     __shared__ float buf[7 * WAVES], p_at[RN50_TOPK_MAX];
-    __shared__ int class_at[RN50_TOPK_MAX], label_kept;
+    __shared__ __align__(16) int class_at[RN50_TOPK_MAX];
+    __shared__ int label_kept;
     const int n = blockIdx.x / grad_parts, s = blockIdx.x % grad_parts, first = s * a.per, tid = threadIdx.x, K = a.K;
     const T *row = z + n * a.ld;
     const float nan = __builtin_nanf("");
@@ -205,7 +226,7 @@ __global__ __launch_bounds__(TH) void distill_kernel(DistillArgs a, int grad_par
                 q[2] = fmaf(st.z, exp2_fast((st.x - mx) * a.ct), q[2]);
             }
     } else {
-        part.sums(mx, ca, a.ct, two, q[1], q[2]);
+        part.sums(mx, ca, a.ct, a.tau, two, q[1], q[2]);
     }
     block_reduce<3, WAVES>(q, buf + 2 * WAVES, Sum());
     const float sa = q[1], st = two ? q[2] : sa, pt = kept ? q[0] == q[0] ? exp2_fast((v - m[0]) * a.ct) / q[0] : nan : 0.f;
@@ -214,7 +235,7 @@ __global__ __launch_bounds__(TH) void distill_kernel(DistillArgs a, int grad_par
     else if (kept && pt != 0.f)
         l[0] = pt * (((v - m[0]) * a.ct - (z_kept - mx) * a.ct) * kLn2 - (logf(q[0]) - logf(st)));
     if (class_ok && k == label) label_kept = 1;
-    if (tid < a.t) {
+    if (tid < RN50_TOPK_MAX) {
         p_at[tid] = pt;
         class_at[tid] = class_ok ? k : -1;
     }
@@ -233,29 +254,40 @@ __global__ __launch_bounds__(TH) void distill_kernel(DistillArgs a, int grad_par
         const float d = x - mx, g = exp2_fast(d * ca) * ka;
         return two ? fmaf(exp2_fast(d * cb), kb, g) : g;
     };
-    // a kept class in this part: the first entry of it writes for all of them
-    float kept_sum = 0.f;
+    // a kept class in this part; where it is there several times, the first entry writes for all of them
+    float kept_sum = pt;
     bool writes = class_ok && (unsigned)(k - first) < (unsigned)len;
-    if (__ballot(writes))
-        for (int i = 0; i < a.t; ++i)
-            if (class_at[i] == k) {
-                writes = writes && i >= tid;
-                kept_sum += p_at[i];
-            }
+    if (__ballot(writes)) {
+        int same = 0;
+        for (int i = 0; i < a.t; i += 4) {
+            const int4 c = *reinterpret_cast<const int4 *>(class_at + i);
+            same += (c.x == k) + (c.y == k) + (c.z == k) + (c.w == k);
+        }
+        if (writes && same > 1) {
+            kept_sum = 0.f;
+            for (int i = 0; i < a.t; ++i)
+                if (class_at[i] == k) {
+                    writes = writes && i >= tid;
+                    kept_sum += p_at[i];
+                }
+        }
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int at = (e * TH + tid) * VEC;
         if (at < whole) {
-            float f[VEC], g[VEC];
+            float f[VEC], g[VEC], h[VEC];
             row_unpack<T, VEC>(part.raw[e], f);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                f[i] -= mx;
-                g[i] = exp2_fast(f[i] * ca) * ka;
-            }
-            if (two)
+            for (int i = 0; i < VEC; ++i) f[i] -= mx;
+            if (two) {
+                two_exps<VEC>(f, ca, cb, a.tau, g, h);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) g[i] = fmaf(exp2_fast(f[i] * cb), kb, g[i]);
+                for (int i = 0; i < VEC; ++i) g[i] = fmaf(h[i], kb, g[i] * ka);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) g[i] = exp2_fast(f[i] * ca) * ka;
+            }
             row_store16(out + at, row_pack<T, VEC>(g));
         }
     }
@@ -302,13 +334,13 @@ __global__ __launch_bounds__(kLossThreads) void distill_loss_kernel(int N, float
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------------
-// One part where a workgroup of 1024 threads holds the row (in vectors of 16 bytes, eight to a thread) and the rows fill the chip; few
-// long rows in parts of 4096 elements or more.
+// One part where a workgroup of 512 threads holds the row (in vectors of 16 bytes, 16 to a thread) and the rows fill the chip.  Longer
+// rows in parts of half of that, which leave a compute unit room for three workgroups; few long rows in parts of 4096 elements or more.
 struct DistillCut { int parts, per; };
 static DistillCut distill_cut(int n, int k, int vec)
 {
     constexpr int kLeast = 4096, kWorkgroups = 512;
-    long parts = ceil_div(k, 1024L * 8 * vec);
+    long parts = k <= 512L * 16 * vec ? 1 : ceil_div(k, 512L * 8 * vec);
     const long wanted = kWorkgroups / n, most = ceil_div(k, kLeast);
     if (parts < wanted) parts = wanted < most ? wanted : most;
     if (parts < 1) parts = 1;
@@ -363,7 +395,7 @@ static int distill_impl(const char *who, int n, int k, int t, const T *logits, s
         constexpr int TH = decltype(threads)::value, E = decltype(vectors)::value;
         if (cut.parts == 1) {
             hipLaunchKernelGGL((distill_kernel<T, TH, E, false>), dim3(n), dim3(TH), 0, st, a, 1, logits, nullptr, dlogits, row_loss);
-        } else {
+        } else if constexpr (E <= 8) {  // distill_cut's parts are no larger
             hipLaunchKernelGGL((distill_stats_kernel<T, TH, E>), dim3((unsigned)((long)n * cut.parts)), dim3(TH), 0, st, a, logits, stats);
             const int grad_parts = dlogits ? cut.parts : 1;
             hipLaunchKernelGGL((distill_kernel<T, TH, E, true>), dim3((unsigned)((long)n * grad_parts)), dim3(TH), 0, st, a, grad_parts, logits, stats, dlogits,
@@ -374,7 +406,7 @@ static int distill_impl(const char *who, int n, int k, int t, const T *logits, s
     if (cut.per <= 256 * VEC) launch(integral_constant<int, 256>{}, integral_constant<int, 1>{});
     else if (cut.per <= 1024 * VEC) launch(integral_constant<int, 256>{}, integral_constant<int, 4>{});
     else if (cut.per <= 4096 * VEC) launch(integral_constant<int, 512>{}, integral_constant<int, 8>{});
-    else launch(integral_constant<int, 1024>{}, integral_constant<int, 8>{});
+    else launch(integral_constant<int, 512>{}, integral_constant<int, 16>{});
     hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(kLossThreads), 0, st, n, alpha, scale, row_loss, loss);
     return launch_status(who);
 }
