@@ -158,7 +158,8 @@ def _ptr(t):
 
 
 def _stream(stream=None):
-    return stream if stream is not None else torch.cuda.current_stream().cuda_stream
+    # the handle of torch.cuda.current_stream(), without the Stream object made around it (2.6 us of a small call's 10)
+    return stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def conv_desc(n, c, h, w, k, r, s, stride, pad, layout=LAYOUT_NHWC, in_dtype=DTYPE_F32):
