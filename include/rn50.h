@@ -342,7 +342,7 @@ int bn_bwd_batchstats(int n, int c, int h, int w, int layout,
  * x, y, residual, dy, dy2, dx, dresidual: N x H x W x C (the _bf16 calls: bfloat16 bits, widened exactly on load, all
  * arithmetic and every sum fp32, one rounding to nearest even per stored value).  gamma, beta, dgamma, dbeta: C floats;
  * save_mean, save_invstd: N x groups floats (both NULL where no backward pass follows).  C % 4 == 0, C % groups == 0,
- * H*W*C and N*C below 2^31 (else RN50_EUNSUPPORTED; groups that do not divide C: RN50_EINVAL).  Outputs do not overlap
+ * C at most 2^20, H*W*C and N*C below 2^31 (else RN50_EUNSUPPORTED; groups that do not divide C: RN50_EINVAL).  Outputs do not overlap
  * inputs.  A NaN or an infinity in a group makes that group's outputs NaN and no other's.  Results are bit-identical
  * from call to call.
  * ------------------------------------------------------------------------------------------ */

@@ -160,11 +160,27 @@ template <int V> __device__ inline void gn_column_sums(const GnMap &m, const GnT
         for (int i = 0; i < V; ++i) part[t.slot * W + t.col * V + i] = v[i];
     __syncthreads();
     for (int c = threadIdx.x; c < W; c += blockDim.x) {
-        float s = part[c];
-        for (int k = 1; k < m.slots; ++k) s += part[k * W + c];
-        out[c] = s;
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        int k = 0;
+        for (; k + 4 <= m.slots; k += 4)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s[u] += part[(k + u) * W + c];
+        for (; k < m.slots; ++k) s[0] += part[k * W + c];
+        out[c] = (s[0] + s[1]) + (s[2] + s[3]);
     }
     __syncthreads();
+}
+// The sum of v over the workgroup, in every thread (red: a float to a wavefront, which no call nearby uses).
+__device__ inline float gn_total(float v, float *red)
+{
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (unsigned k = 0; k < blockDim.x / 64; k += 4)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[u] += red[k + u];
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 // Sums of runs of `run` of the W channels: groups[i] = sum of chan[i*run ..].  Few long runs: each the whole workgroup's work.  Ends with
 // a barrier.
@@ -185,9 +201,13 @@ __device__ inline void gn_group_sums(int W, int run, const float *chan, float *g
         }
     } else {
         for (int g = threadIdx.x; g < W / run; g += blockDim.x) {
-            float s = 0.f;
-            for (int i = 0; i < run; ++i) s += chan[g * run + i];
-            groups[g] = s;
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+            int i = 0;
+            for (; i + 4 <= run; i += 4)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) s[u] += chan[g * run + i + u];
+            for (; i < run; ++i) s[0] += chan[g * run + i];
+            groups[g] = (s[0] + s[1]) + (s[2] + s[3]);
         }
     }
     __syncthreads();
@@ -197,6 +217,29 @@ struct GnShape {
     int HW, C, G, Cg;
     int n0;  // first image of the launch
 };
+// Both of a thread's sums by column, a0 and a1, left in chan: W values of the one, W of the other (part: 2 * slots * W floats).  f(c, s0, s1)
+// sees channel c's and returns what stays of them.  Then their sums by group in grp: W/run of the one, W/run of the other.
+template <int V, class F>
+__device__ inline void gn_two_sums(const GnMap &m, const GnThread &t, const float (&a0)[V], const float (&a1)[V], int width, int run, float *part,
+                                   float *chan, float *grp, float *red, F f)
+{
+    float both[2 * V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        both[i] = a0[i];
+        both[V + i] = a1[i];
+    }
+    gn_column_sums<2 * V>(m, t, both, part, grp);  // column by column, a0's and a1's side by side
+    for (int c = threadIdx.x; c < width; c += blockDim.x) {
+        const int at = c / V * 2 * V + c % V;
+        const float2 kept = f(c, grp[at], grp[at + V]);
+        chan[c] = kept.x;
+        chan[width + c] = kept.y;
+    }
+    __syncthreads();
+    gn_group_sums(2 * width, run, chan, grp, red);
+}
+
 // S values of a vector that differ by group: one where vectors lie within groups (S == 1), else one to a channel.  Index of channel i's.
 template <int S> __device__ constexpr int gn_at(int i) { return S == 1 ? 0 : i; }
 
@@ -206,8 +249,8 @@ struct GnResident {
     int W, chunks;  // channels of a workgroup, and how many such to an image
 };
 
-// LDS: slots*W partial sums, W sums by channel, sums by group
-static size_t gn_lds_floats(const GnMap &m, int W, int planes) { return (size_t)planes * (m.slots * W + W) + 16 + planes * (size_t)W; }
+// LDS: slots*W partial sums, W sums by channel, of each kind; a float to a wavefront, twice; sums by group (or column)
+static size_t gn_lds_floats(const GnMap &m, int W, int planes) { return (size_t)planes * (m.slots * W + 2 * W) + 32; }
 
 template <class T, int V, int S, int E, int TH, int ACT, bool RES>
 __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, const T *__restrict__ x, const float *__restrict__ gamma,
@@ -217,7 +260,7 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
     typedef GnVec<T, V> Vec;
     constexpr int PER = V / S;  // channels of a thread that share statistics
     extern __shared__ float lds[];
-    float *part = lds, *chan = part + p.map.slots * p.W, *red = chan + p.W, *grp = red + 16;
+    float *part = lds, *chan = part + p.map.slots * p.W, *red = chan + p.W, *grp = red + 32;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);
     const int n = s.n0 + id / p.chunks, c0 = id % p.chunks * p.W;
     const GnThread t(p.map);
@@ -238,12 +281,23 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
 #pragma unroll
             for (int i = 0; i < V; ++i) a[gn_at<S>(i)] += f[i];
         }
-    gn_column_sums<S>(p.map, t, a, part, chan);
-    gn_group_sums(p.W / PER, s.Cg / PER, chan, grp, red);
+    // sums by group; a workgroup of one group needs no columns
+    const bool one = S == 1 && p.W == s.Cg;
+    auto by_group = [&](float (&v)[S], float *spare) {
+        if (one) {
+            v[0] = gn_total(v[0], spare);
+            return;
+        }
+        gn_column_sums<S>(p.map, t, v, part, chan);
+        gn_group_sums(p.W / PER, s.Cg / PER, chan, grp, red);
+#pragma unroll
+        for (int i = 0; i < S; ++i) v[i] = grp[(col + i) / s.Cg];
+    };
+    by_group(a, red);
     const float m = (float)s.HW * (float)s.Cg;  // a division: the mean of equal values is that value, whatever their number
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-        mean[i] = grp[(col + i) / s.Cg] / m;
+        mean[i] = a[i] / m;
         a[i] = 0.f;
     }
 #pragma unroll
@@ -257,15 +311,14 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
                 a[gn_at<S>(i)] = fmaf(d, d, a[gn_at<S>(i)]);
             }
         }
-    gn_column_sums<S>(p.map, t, a, part, chan);  // its first barrier: every thread has read grp
-    gn_group_sums(p.W / PER, s.Cg / PER, chan, grp, red);
+    by_group(a, red + 16);  // by columns: the first barrier says that every thread has read grp
     if (!t.active) return;
     float scale[V], b[V], invstd[S];
     gn_load_floats<V>(gamma + c, scale);
     gn_load_floats<V>(beta + c, b);
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-        invstd[i] = 1.f / sqrtf(grp[(col + i) / s.Cg] / m + eps);
+        invstd[i] = 1.f / sqrtf(a[i] / m + eps);
         if (save_mean && t.row == 0 && (c + i) % s.Cg == 0) {
             save_mean[(long)n * s.G + (c + i) / s.Cg] = mean[i];
             save_invstd[(long)n * s.G + (c + i) / s.Cg] = invstd[i];
@@ -368,8 +421,7 @@ __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, lon
 {
     typedef GnVec<T, V> Vec;
     extern __shared__ float lds[];
-    const int plane = p.map.slots * p.W;
-    float *part0 = lds, *part1 = part0 + plane, *chan0 = part1 + plane, *chan1 = chan0 + p.W, *red = chan1 + p.W, *grp0 = red + 16, *grp1 = grp0 + p.W;
+    float *part = lds, *chan = part + 2 * p.map.slots * p.W, *red = chan + 2 * p.W, *grp = red + 32;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);
     const int n = s.n0 + id / p.chunks, c0 = id % p.chunks * p.W;
     const GnThread t(p.map);
@@ -400,23 +452,18 @@ __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, lon
                 }
             }
     }
-    gn_column_sums<V>(p.map, t, a0, part0, chan0);
-    gn_column_sums<V>(p.map, t, a1, part1, chan1);
-    for (int i = threadIdx.x; i < p.W; i += TH) {
-        const float s0 = chan0[i], s1 = chan1[i], g = in.gamma[c0 + i];
+    gn_two_sums<V>(p.map, t, a0, a1, p.W, s.Cg, part, chan, grp, red, [&](int i, float s0, float s1) {
         sums[(long)n * s.C + c0 + i] = s0;
         sums[NC + (long)n * s.C + c0 + i] = s1;
-        chan0[i] = s0 * g;
-        chan1[i] = s1 * g;
-    }
-    __syncthreads();
-    gn_group_sums(p.W, s.Cg, chan0, grp0, red);
-    gn_group_sums(p.W, s.Cg, chan1, grp1, red);
+        const float g = in.gamma[c0 + i];
+        return make_float2(s0 * g, s1 * g);
+    });
+    const float *grp1 = grp + p.W / s.Cg;
     const float m = (float)s.HW * (float)s.Cg;
     float A[S], Bm[S];
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-        A[i] = grp0[(col + i) / s.Cg] / m * k.inv[i];
+        A[i] = grp[(col + i) / s.Cg] / m * k.inv[i];
         Bm[i] = grp1[(col + i) / s.Cg] / m * k.inv[i];
     }
 #pragma unroll
@@ -495,7 +542,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnShape s, GnBands
     constexpr int PER = V / S;  // channels of a thread that share statistics
     extern __shared__ float lds[];
     const int sums = p.map.cols * S;  // a row's partial sums
-    float *part = lds, *chan = part + p.map.slots * sums, *red = chan + sums, *grp = red + 16;
+    float *part = lds, *chan = part + p.map.slots * sums, *red = chan + sums, *grp = red + 32;
     const GnPlace pl(s, p, blockIdx.x, gridDim.x, false);
     GnThread t(p.map);
     t.active = t.active && t.col * V < pl.width;
@@ -645,7 +692,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape s, GnBands 
                                                              float *__restrict__ parts)
 {
     extern __shared__ float lds[];
-    float *part = lds, *chan0 = part + p.map.slots * p.W, *chan1 = chan0 + p.W, *red = chan1 + p.W, *grp = red + 16;
+    float *part = lds, *chan = part + 2 * p.map.slots * p.W, *red = chan + 2 * p.W, *grp = red + 32;
     const GnPlace pl(s, p, blockIdx.x, gridDim.x, false);
     GnThread t(p.map);
     t.active = t.active && t.col * V < pl.width;
@@ -674,22 +721,15 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape s, GnBands 
                     }
                 }
         }
-    gn_column_sums<V>(p.map, t, a0, part, chan0);
-    gn_column_sums<V>(p.map, t, a1, part, chan1);
     float *out = chans + ((long)n * p.bands + pl.band) * s.C + pl.c0;
-    for (int i = threadIdx.x; i < pl.width; i += kGnThreads) {
+    gn_two_sums<V>(p.map, t, a0, a1, pl.width, pl.run, part, chan, grp, red, [&](int i, float s0, float s1) {
+        out[i] = s0;
+        out[chan_plane + i] = s1;
         const float g = in.gamma[pl.c0 + i];
-        out[i] = chan0[i];
-        out[chan_plane + i] = chan1[i];
-        chan0[i] *= g;
-        chan1[i] *= g;
-    }
-    __syncthreads();
+        return make_float2(s0 * g, s1 * g);
+    });
     const int count = pl.width / pl.run;
-    gn_group_sums(pl.width, pl.run, chan0, grp, red);
-    for (int i = threadIdx.x; i < count; i += kGnThreads) *pl.partial(s, p, parts, i) = grp[i];
-    gn_group_sums(pl.width, pl.run, chan1, grp + count, red);
-    for (int i = threadIdx.x; i < count; i += kGnThreads) *pl.partial(s, p, parts + p.plane, i) = grp[count + i];
+    for (int i = threadIdx.x; i < 2 * count; i += kGnThreads) *pl.partial(s, p, parts + (i < count ? 0 : p.plane), i < count ? i : i - count) = grp[i];
 }
 
 // The group's means of gamma*dz and gamma*dz*xhat, from its bands' sums.
@@ -859,6 +899,7 @@ static GnRoom gn_room(int n, int c, int HW, int groups)
     return r;
 }
 
+constexpr int kGnMaxChannels = 1 << 20;  // an image's workgroups have fewer than 2^32 threads
 static int gn_check(const char *who, int n, int c, int h, int w, int layout, int groups, int act)
 {
     RN50_REQUIRE(n > 0 && c > 0 && h > 0 && w > 0 && groups > 0, RN50_EINVAL, "%s: non-positive dimension", who);
@@ -866,6 +907,7 @@ static int gn_check(const char *who, int n, int c, int h, int w, int layout, int
     RN50_REQUIRE(c % 4 == 0, RN50_EUNSUPPORTED, "%s: channel count must be a multiple of 4", who);
     RN50_REQUIRE(c % groups == 0, RN50_EINVAL, "%s: groups must divide the channel count", who);
     RN50_REQUIRE(act >= RN50_ACT_NONE && act <= RN50_ACT_SILU, RN50_EINVAL, "%s: unknown activation", who);
+    RN50_REQUIRE(c <= kGnMaxChannels, RN50_EUNSUPPORTED, "%s: more than 2^20 channels", who);
     RN50_REQUIRE((long)h * w < (1L << 31) && (long)h * w * c < (1L << 31) && (long)n * c < (1L << 31), RN50_EUNSUPPORTED,
                  "%s: H*W*C and N*C must be below 2^31", who);
     return RN50_OK;
@@ -955,8 +997,9 @@ static int gn_fwd_impl(const char *who, int n, int c, int h, int w, int layout, 
         const GnBands p = gn_bands(n, HW, c, Cg, V, gn_reduce_total(n)), pa = gn_bands(n, HW, c, Cg, V, gn_apply_total());
         float *mean = save_mean ? save_mean : (float *)ws, *invstd = save_invstd ? save_invstd : mean + (size_t)n * groups;
         float *parts = (float *)ws + room.pairs;
-        const size_t lds = ((size_t)(p.map.slots + 2) * p.W + 16) * sizeof(float);
-        const int each = gn_images(n, (long)pa.bands * pa.chunks, kGnThreads);  // the finer cut
+        const size_t lds = gn_lds_floats(p.map, p.W, 1) * sizeof(float);
+        const long finest = (long)pa.bands * pa.chunks;
+        const int each = gn_images(n, finest > groups ? finest : groups, kGnThreads);
         for (int n0 = 0; n0 < n; n0 += each) {
             const int images = n - n0 < each ? n - n0 : each;
             const GnShape s{HW, c, groups, Cg, n0};
@@ -1023,8 +1066,9 @@ static int gn_bwd_impl(const char *who, int n, int c, int h, int w, int layout, 
         }
         const GnBands p = gn_bands(n, HW, c, Cg, V, gn_reduce_total(n)), pa = gn_bands(n, HW, c, Cg, V, gn_apply_total());
         const long rows = (long)n * p.bands;
-        const size_t lds = ((size_t)(p.map.slots + 4) * p.W + 16) * sizeof(float);
-        const int each = gn_images(n, (long)pa.bands * pa.chunks, kGnThreads);  // the finer cut
+        const size_t lds = gn_lds_floats(p.map, p.W, 2) * sizeof(float);
+        const long finest = (long)pa.bands * pa.chunks;
+        const int each = gn_images(n, finest > groups ? finest : groups, kGnThreads);
         for (int n0 = 0; n0 < n; n0 += each) {
             const int images = n - n0 < each ? n - n0 : each, blocks = images * p.bands * p.chunks, finer = images * pa.bands * pa.chunks;
             const int params = n0 + images == n ? param_blocks : 0;  // with the last launch
@@ -1048,7 +1092,7 @@ using namespace rn50;
 
 extern "C" size_t rn50_gn_workspace_bytes(int n, int c, int h, int w, int groups)
 {
-    if (n <= 0 || c <= 0 || h <= 0 || w <= 0 || groups <= 0 || c % 4 || c % groups || (long)h * w >= (1L << 31) || (long)h * w * c >= (1L << 31) ||
+    if (n <= 0 || c <= 0 || h <= 0 || w <= 0 || groups <= 0 || c % 4 || c % groups || c > kGnMaxChannels || (long)h * w >= (1L << 31) || (long)h * w * c >= (1L << 31) ||
         (long)n * c >= (1L << 31))
         return 0;
     return gn_room(n, c, h * w, groups).floats() * sizeof(float);

@@ -251,7 +251,10 @@ __global__ __launch_bounds__(TH) void topk_kernel(int K, int t, int parts, int p
         }
         for (int i = threadIdx.x; i < len; i += TH) {
             const uint32_t o = Word::order(row[i]);
-            if (o > L || (o == L && (uint32_t)i <= last)) found[atomicAdd(&total[2], 1)] = topk_pair(o, first + i);
+            if (o > L || (o == L && (uint32_t)i <= last)) {
+                const int slot = atomicAdd(&total[2], 1);
+                if (slot < kTopkFound) found[slot] = topk_pair(o, first + i);  // t of them, unless someone writes the row meanwhile
+            }
         }
         __syncthreads();
         all = t;

@@ -23,7 +23,7 @@ GN_BOTH = [(dict(n=0), rn.EINVAL), (dict(h=-1), rn.EINVAL), (dict(groups=0), rn.
            (dict(c=6, groups=2), rn.EUNSUPPORTED), (dict(layout=rn.LAYOUT_NCHW), rn.EUNSUPPORTED), (dict(act=3), rn.EINVAL), (dict(act=-1), rn.EINVAL),
            (dict(x=None), rn.EINVAL), (dict(gamma=None), rn.EINVAL), (dict(beta=None), rn.EINVAL), (dict(ws=None), rn.EINVAL),
            (dict(x=P[0] + 4), rn.EINVAL), (dict(res=P[3] + 8), rn.EINVAL), (dict(ws=P[7] + 2), rn.EINVAL), (dict(nbytes=0), rn.EWORKSPACE),
-           (dict(h=1 << 16, w=1 << 15), rn.EUNSUPPORTED), (dict(h=1 << 14, w=1 << 14), rn.EUNSUPPORTED), (dict(n=1 << 29), rn.EUNSUPPORTED)]
+           (dict(h=1 << 16, w=1 << 15), rn.EUNSUPPORTED), (dict(h=1 << 14, w=1 << 14), rn.EUNSUPPORTED), (dict(n=1 << 29), rn.EUNSUPPORTED), (dict(c=(1 << 20) + 4, h=1, w=1), rn.EUNSUPPORTED)]
 
 
 @pytest.mark.parametrize("suffix", ["", "_bf16"])
@@ -41,7 +41,7 @@ def test_group_norm_refusals(suffix):
 
 def test_group_norm_workspace_query():
     assert rn.rn50_gn_workspace_bytes(32, 64, 112, 112, 32) >= 2 * 4 * 32 * 64
-    for bad in ((0, 8, 3, 5, 4), (2, 6, 3, 5, 2), (2, 8, 3, 5, 3), (2, 8, 3, 5, 0), (2, 8, 1 << 16, 1 << 15, 4), (1 << 29, 8, 1, 1, 4)):
+    for bad in ((0, 8, 3, 5, 4), (2, 6, 3, 5, 2), (2, 8, 3, 5, 3), (2, 8, 3, 5, 0), (2, 8, 1 << 16, 1 << 15, 4), (1 << 29, 8, 1, 1, 4), (1, (1 << 20) + 4, 1, 1, 4)):
         assert rn.rn50_gn_workspace_bytes(*bad) == 0, bad
 
 
@@ -55,14 +55,16 @@ def test_topk_refusals(suffix):
     for args, code in [(dict(n=0), rn.EINVAL), (dict(k=0), rn.EINVAL), (dict(t=0), rn.EINVAL), (dict(t=11), rn.EINVAL), (dict(ld=9), rn.EINVAL),
                        (dict(k=1000, ld=1000, t=257), rn.EUNSUPPORTED), (dict(n=1 << 22), rn.EUNSUPPORTED), (dict(ld=1 << 31), rn.EINVAL),
                        (dict(z=None), rn.EINVAL), (dict(val=None), rn.EINVAL), (dict(idx=None), rn.EINVAL), (dict(z=P[0] + 4), rn.EINVAL),
-                       (dict(val=P[1] + 8), rn.EINVAL), (dict(idx=P[2] + 4), rn.EINVAL), (dict(ws=P[3] + 4), rn.EINVAL)]:
+                       (dict(val=P[1] + 8), rn.EINVAL), (dict(idx=P[2] + 4), rn.EINVAL), (dict(ws=P[3] + 4), rn.EINVAL),
+                       (dict(n=1, k=(24 << 15) + 1, ld=1 << 20, t=256), rn.EUNSUPPORTED), (dict(n=1 << 20, k=1 << 18, ld=1 << 18), rn.EUNSUPPORTED)]:
         assert _topk(L, fn="logits_topk" + suffix, **args) == code, args
     need = rn.rn50_topk_workspace_bytes(1, 131072, 256)
     if need:
         args = dict(n=1, k=131072, ld=131072, t=256)
         assert _topk(L, fn="logits_topk" + suffix, nbytes=need - 1, **args) == rn.EWORKSPACE
         assert _topk(L, fn="logits_topk" + suffix, ws=None, nbytes=need, **args) == rn.EINVAL
-    for bad in ((0, 5, 1), (1, 0, 1), (1, 5, 0), (1, 5, 6)):
+    assert rn.rn50_topk_workspace_bytes(1, 24 << 15, 256) > 0
+    for bad in ((0, 5, 1), (1, 0, 1), (1, 5, 0), (1, 5, 6), (1, (24 << 15) + 1, 256)):
         assert rn.rn50_topk_workspace_bytes(*bad) == 0, bad
 
 
@@ -81,7 +83,8 @@ def test_distillation_refusals(suffix):
                        (dict(alpha=nan), rn.EINVAL), (dict(tau=0.0), rn.EINVAL), (dict(tau=nan), rn.EINVAL), (dict(tau=2000.0), rn.EINVAL),
                        (dict(tau=1e-4), rn.EINVAL), (dict(scale=nan), rn.EINVAL), (dict(scale=inf), rn.EINVAL), (dict(z=None), rn.EINVAL),
                        (dict(labels=None), rn.EINVAL), (dict(idx=None), rn.EINVAL), (dict(val=None), rn.EINVAL), (dict(loss=None), rn.EINVAL),
-                       (dict(ws=None), rn.EINVAL), (dict(dz=P[0]), rn.EINVAL), (dict(nbytes=0), rn.EWORKSPACE)] + \
+                       (dict(ws=None), rn.EINVAL), (dict(dz=P[0]), rn.EINVAL), (dict(nbytes=0), rn.EWORKSPACE),
+                       (dict(n=1 << 20, k=1 << 20, ld=1 << 20, ldd=1 << 20), rn.EUNSUPPORTED)] + \
                       [(dict([(name, P[8] + 4)]), rn.EINVAL) for name in ("z", "labels", "idx", "val", "loss", "dz", "ws")]:
         assert _distill(L, fn="distill_ce" + suffix, **args) == code, args
     need = rn.rn50_distill_workspace_bytes(3, 10, 4)

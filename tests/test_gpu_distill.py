@@ -80,6 +80,58 @@ def test_topk_of_rows_that_are_hard_to_cut(n, k, t, bf16):
         _check_topk(z, t, bf16)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+def test_topk_of_nans_with_either_sign(bf16):
+    """A NaN whose sign bit is set lies where negative numbers do, by its bits."""
+    n, k, t = 6, 3000, 12
+    z = _rows(2, n, k, False)
+    z[0, 77] = z[1, 5] = z[1, 2999] = z[2, :20] = np.copysign(np.float32(np.nan), np.float32(-1))
+    z[1, 2000] = np.nan
+    z[3] = -np.abs(z[3])
+    z[3, 1500] = np.copysign(np.float32(np.nan), np.float32(-1))
+    z[4] = -np.inf
+    z[4, [3, 2998]] = -0.0, np.copysign(np.float32(np.nan), np.float32(-1))
+    assert np.signbit(z[0, 77])
+    dt = torch.bfloat16 if bf16 else torch.float32
+    zd = torch.from_numpy(z).to(DEV)
+    if bf16:   # the upper halves of the bits, so that the signs of the NaNs stay
+        zd = (zd.view(torch.int32) >> 16).to(torch.int16).view(torch.bfloat16)
+    val, idx = torch.empty((n, t), device=DEV), torch.empty((n, t), dtype=torch.int32, device=DEV)
+    (rn.logits_topk_bf16 if bf16 else rn.logits_topk)(n, k, t, zd.contiguous(), k, val, idx, ws_bytes(rn.rn50_topk_workspace_bytes(n, k, t)))
+    rval, ridx = orc.topk(zd.float().cpu().numpy(), t)
+    np.testing.assert_array_equal(idx.cpu().numpy(), ridx)
+    np.testing.assert_array_equal(val.cpu().numpy(), rval.astype(np.float32))
+
+
+@pytest.mark.parametrize("n,k", [(540, 32769), (3, 65536), (530, 65537), (520, 32768), (515, 16385)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_distillation_at_the_lengths_where_rows_are_cut(n, k, bf16):
+    """One part, and two of them, of many rows: a few rows against the oracle, and the loss of all against the rows' own."""
+    t, tau, alpha = 6, 4.0, 0.5
+    g = torch.Generator(device=DEV).manual_seed(k)
+    dt = torch.bfloat16 if bf16 else torch.float32
+    z = (3 * torch.randn((n, k), generator=g, device=DEV)).to(dt)
+    idx = torch.stack([torch.randperm(k, generator=g, device=DEV)[:t] for _ in range(n)]).to(torch.int32)
+    idx[:, 0], idx[:, 1] = 0, k - 1
+    val, labels = torch.randn((n, t), generator=g, device=DEV), torch.randint(0, k, (n,), generator=g, device=DEV, dtype=torch.int32)
+    labels[0], labels[1], labels[2] = k - 1, k // 2, 0
+    loss, dz, ws = torch.empty(3, device=DEV), torch.empty_like(z), ws_bytes(rn.rn50_distill_workspace_bytes(n, k, t))
+    (rn.distill_ce_bf16 if bf16 else rn.distill_ce)(n, k, t, z, k, labels, idx, val, alpha, tau, 1 / n, loss, dz, k, ws)
+    rows = [0, 1, 2, n - 1]
+    zr, lr, ir, vr = z[rows].float().cpu().numpy(), labels[rows].cpu().numpy(), idx[rows].cpu().numpy(), val[rows].cpu().numpy()
+    _, rdz = orc.distill_ce(zr, lr, ir, vr, alpha, tau, 1 / n)
+    _, off = _bounds(zr, lr, ir, vr, alpha, tau, 1 / n)
+    over = np.abs(dz[rows].double().cpu().numpy() - rdz) - off - (2.0 ** -8 * np.abs(rdz) if bf16 else 0) - 1e-37
+    assert over.max() <= 0
+    # the loss of all rows from the float64 softmaxes of torch; a row's terms of 20 are off by some 60 roundings of 2^-24 of it at most
+    zd = z.double()
+    hard = (torch.logsumexp(zd, 1) - zd.gather(1, labels.long()[:, None])[:, 0]).sum() / n
+    p = torch.softmax(val.double() / tau, 1)
+    soft = tau * tau * (p * (torch.log(p) - zd.gather(1, idx.long()) / tau + torch.logsumexp(zd / tau, 1, keepdim=True))).sum() / n
+    for got, ref in zip(loss.tolist(), (0.5 * hard + 0.5 * soft, hard, soft)):
+        assert abs(got - float(ref)) <= 60 * U * (abs(float(ref)) + tau * tau * 20)
+
+
 def test_topk_far_into_memory():
     """Rows that start beyond 2^31 elements."""
     n, k, t, ld = 40, 70001, 9, 1 << 26
