@@ -1,7 +1,7 @@
 // The t largest logits of each row, in order.  One pass over memory: a workgroup keeps its part of a row in registers and finds a bound
 // that at least t elements reach and few more.  Every wavefront's r-th largest of its lanes' own maxima, r = t / wavefronts, is reached by
 // r elements there; the smallest of these bounds over the wavefronts by t in all.  (Random rows of 32768 and t = 64: some 110 elements.)
-// Those go to LDS, and each counts how many are larger: that is its place.
+// Those go to LDS and are sorted there.
 // Where too many reach the bound (equal logits, rows made to defeat it), the t-th largest element itself is found bit by bit.
 // Long rows of which there are few are cut into parts for several workgroups, and the parts' sorted lists merged.
 #include "rows.h"
@@ -90,27 +90,45 @@ __device__ inline int32_t wave_rth_largest(int32_t v, int r, int low)
     return (int32_t)(L ^ 0x80000000u);
 }
 
-constexpr int kTopkFound = 1024;  // elements in LDS
+constexpr int kTopkFound = 1024;  // elements in LDS (a multiple of 64)
 
-// Of `all` pairs in LDS, f(place, pair) for the t largest; place: as many zeros.  Several threads share the counting where there are
-// fewer pairs than threads.
-template <int TH, class F> __device__ inline void topk_places(int t, int all, const uint64_t *found, int *place, F f)
+// How many of 64 falling pairs are larger than `own`.
+__device__ inline int topk_larger(const uint64_t *run, uint64_t own)
 {
-    const int span = (all + 63) & ~63, shares = max(1, TH / span), chunk = (all + shares - 1) / shares;
-    for (int i0 = threadIdx.x; i0 < span * shares; i0 += TH) {
-        const int i = i0 % span, from = i0 / span * chunk, to = min(all, from + chunk);
-        if (i < all) {
-            const uint64_t own = found[i];
-            int c = 0;
-#pragma unroll 4
-            for (int j = from; j < to; ++j) c += found[j] > own;
-            if (shares > 1) atomicAdd(&place[i], c);
-            else place[i] = c;
-        }
+    int at = 0;
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1)
+        if (run[at + step - 1] > own) at += step;
+    return at + (run[at] > own);
+}
+
+// Of `all` pairs in LDS, f(place, pair) for the t largest.  Every wavefront sorts runs of 64 (the exchanges of a bitonic network between
+// lanes), then a pair's place is that in its run and, by bisection, the number of larger ones in each other run.  (1024 rows of 65536 fp32,
+// t = 256, some 450 pairs in each of two parts: 91 us; each pair counting the larger ones among all: 145.)
+template <int TH, class F> __device__ inline void topk_places(int t, int all, uint64_t *found, F f)
+{
+    const int runs = (all + 63) / 64, lane = threadIdx.x & 63;
+    for (int run = threadIdx.x >> 6; run < runs; run += TH / 64) {
+        uint64_t own = run * 64 + lane < all ? found[run * 64 + lane] : 0;
+#pragma unroll
+        for (int size = 2; size <= 64; size *= 2)
+#pragma unroll
+            for (int step = size / 2; step > 0; step /= 2) {
+                const uint64_t other = __shfl_xor((unsigned long long)own, step, 64);
+                const bool larger = ((lane & step) == 0) == ((lane & size) == 0);  // this lane keeps the larger one
+                own = (other > own) == larger ? other : own;
+            }
+        found[run * 64 + lane] = own;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < all; i += TH)
-        if (place[i] < t) f(place[i], found[i]);
+    for (int i = threadIdx.x; i < runs * 64; i += TH) {
+        const uint64_t own = found[i];
+        if (own == 0) continue;  // no pair: the last run's, behind its pairs
+        int p = i & 63;
+        for (int run = 0; run < runs; ++run)
+            if (run != i >> 6) p += topk_larger(found + run * 64, own);
+        if (p < t) f(p, own);
+    }
 }
 
 // Part s of row n: `per` elements from s*per (a multiple of the vector).  One part: val and idx; several: pairs, [row][part][t], zeros
@@ -122,7 +140,6 @@ __global__ __launch_bounds__(TH) void topk_kernel(int K, int t, int parts, int p
     typedef TopkWord<T> Word;
     constexpr int PER = Word::PER, VEC = 4 * PER, WAVES = TH / 64;
     __shared__ __align__(16) uint64_t found[kTopkFound];
-    __shared__ int place[kTopkFound];
     __shared__ int32_t bound[2][WAVES];
     __shared__ int counts[2][WAVES], total[3];
     const int n = blockIdx.x / parts, s = blockIdx.x % parts, first = s * per, len = min(per, K - first);
@@ -153,7 +170,6 @@ __global__ __launch_bounds__(TH) void topk_kernel(int K, int t, int parts, int p
         w[e][0] = raw.x; w[e][1] = raw.y; w[e][2] = raw.z; w[e][3] = raw.w;
     }
     if (threadIdx.x < 3) total[threadIdx.x] = 0;
-    for (int i = threadIdx.x; i < kTopkFound; i += TH) place[i] = 0;
     // wavefronts all of whose lanes have a vector (or the first): they make the bound
     const int full = max(1, min(WAVES, (len + VEC - 1) / VEC / 64)), r = (t + full - 1) / full;
     int all = kTopkFound + 1;
@@ -259,7 +275,7 @@ __global__ __launch_bounds__(TH) void topk_kernel(int K, int t, int parts, int p
         __syncthreads();
         all = t;
     }
-    topk_places<TH>(t, all, found, place, [&](int p, uint64_t pair) {
+    topk_places<TH>(t, all, found, [&](int p, uint64_t pair) {
         if (parts > 1) {
             pairs[((size_t)n * parts + s) * t + p] = pair;
         } else {
@@ -278,10 +294,9 @@ __global__ __launch_bounds__(kTopkMergeThreads) void topk_merge_kernel(int t, in
                                                                        int32_t *__restrict__ idx)
 {
     __shared__ uint64_t list[kTopkMergeMost], found[kTopkFound];
-    __shared__ int place[kTopkFound], total;
+    __shared__ int total;
     const int n = blockIdx.x, all = parts * t, lane = threadIdx.x & 63;
     for (int i = threadIdx.x; i < all; i += kTopkMergeThreads) list[i] = pairs[(size_t)n * all + i];
-    for (int i = threadIdx.x; i < kTopkFound; i += kTopkMergeThreads) place[i] = 0;
     if (threadIdx.x == 0) total = 0;
     __syncthreads();
     const int r = (t + parts - 1) / parts;
@@ -300,7 +315,7 @@ __global__ __launch_bounds__(kTopkMergeThreads) void topk_merge_kernel(int t, in
         val[(size_t)n * t + p] = topk_value((uint32_t)(pair >> 32));
         idx[(size_t)n * t + p] = topk_class(pair);
     };
-    if (total <= kTopkFound) return topk_places<kTopkMergeThreads>(t, total, found, place, put);
+    if (total <= kTopkFound) return topk_places<kTopkMergeThreads>(t, total, found, put);
     for (int i = threadIdx.x; i < all; i += kTopkMergeThreads) {
         const uint64_t own = list[i];
         if (own < L) continue;
