@@ -4,6 +4,8 @@
 // Those go to LDS and are sorted there.
 // Where too many reach the bound (equal logits, rows made to defeat it), the t-th largest element itself is found bit by bit.
 // Long rows of which there are few are cut into parts for several workgroups, and the parts' sorted lists merged.
+// 4096 rows of 32768 bf16, t = 64: 62 us, 4.3 TB/s (a row's loads, bound, and sorting wait for each other; three rows to a compute unit
+// overlap).  With workgroups of 1024 threads, of which one fits, 116.
 #include "rows.h"
 
 namespace rn50 {
