@@ -407,11 +407,12 @@ ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 TOPK_MAX = 256
 
 
-def _arg(t, dev, count, dtype):
-    """Pointer of a tensor (None: NULL) that has to hold at least `count` elements of `dtype` on the GPU `dev`, the current one, where the call launches."""
+def _arg(t, dev, count, dtype=None):
+    """Pointer of a tensor (None: NULL) that has to hold at least `count` elements of `dtype` (None: any) on the GPU `dev`, the current one,
+    where the call launches."""
     if t is None:
         return None
-    assert t.get_device() == dev and t.is_contiguous() and t.dtype is dtype and t.numel() >= count, \
+    assert t.get_device() == dev and t.is_contiguous() and (dtype is None or t.dtype is dtype) and t.numel() >= count, \
         "wanted: a contiguous %s tensor of %d elements on the current GPU" % (dtype, count)
     return t.data_ptr()
 
@@ -423,7 +424,7 @@ def rn50_gn_workspace_bytes(n, c, h, w, groups):
 def _gn_fwd(fn, dt, n, c, h, w, groups, x, gamma, beta, eps, residual, act, y, save_mean, save_invstd, ws, stream, layout):
     f32, size, stats, dev = torch.float32, n * c * h * w, n * groups, torch.cuda.current_device()
     _check(fn(n, c, h, w, layout, groups, _arg(x, dev, size, dt), _arg(gamma, dev, c, f32), _arg(beta, dev, c, f32), eps, _arg(residual, dev, size, dt), act,
-              _arg(y, dev, size, dt), _arg(save_mean, dev, stats, f32), _arg(save_invstd, dev, stats, f32), _ptr(ws), _bytes(ws), _stream(stream)))
+              _arg(y, dev, size, dt), _arg(save_mean, dev, stats, f32), _arg(save_invstd, dev, stats, f32), _arg(ws, dev, 0), _bytes(ws), _stream(stream)))
 
 
 def gn_fwd(n, c, h, w, groups, x, gamma, beta, eps, residual, act, y, save_mean, save_invstd, ws, stream=None, layout=LAYOUT_NHWC):
@@ -439,7 +440,7 @@ def _gn_bwd(fn, dt, n, c, h, w, groups, x, dy, dy2, residual, gamma, beta, save_
     f32, size, stats, dev = torch.float32, n * c * h * w, n * groups, torch.cuda.current_device()
     _check(fn(n, c, h, w, layout, groups, _arg(x, dev, size, dt), _arg(dy, dev, size, dt), _arg(dy2, dev, size, dt), _arg(residual, dev, size, dt),
               _arg(gamma, dev, c, f32), _arg(beta, dev, c, f32), _arg(save_mean, dev, stats, f32), _arg(save_invstd, dev, stats, f32), act, _arg(dx, dev, size, dt),
-              _arg(dresidual, dev, size, dt), _arg(dgamma, dev, c, f32), _arg(dbeta, dev, c, f32), _ptr(ws), _bytes(ws), _stream(stream)))
+              _arg(dresidual, dev, size, dt), _arg(dgamma, dev, c, f32), _arg(dbeta, dev, c, f32), _arg(ws, dev, 0), _bytes(ws), _stream(stream)))
 
 
 def gn_bwd(n, c, h, w, groups, x, dy, dy2, residual, gamma, beta, save_mean, save_invstd, act, dx, dresidual, dgamma, dbeta, ws, stream=None,
@@ -460,7 +461,7 @@ def rn50_topk_workspace_bytes(n, k, t):
 
 def _topk(fn, dt, n, k, t, logits, ld, val, idx, ws, stream):
     dev = torch.cuda.current_device()
-    _check(fn(n, k, t, _arg(logits, dev, (n - 1) * ld + k, dt), ld, _arg(val, dev, n * t, torch.float32), _arg(idx, dev, n * t, torch.int32), _ptr(ws),
+    _check(fn(n, k, t, _arg(logits, dev, (n - 1) * ld + k, dt), ld, _arg(val, dev, n * t, torch.float32), _arg(idx, dev, n * t, torch.int32), _arg(ws, dev, 0),
               _bytes(ws), _stream(stream)))
 
 
@@ -479,7 +480,7 @@ def rn50_distill_workspace_bytes(n, k, t):
 def _distill(fn, dt, n, k, t, logits, ld, labels, teacher_idx, teacher_val, alpha, tau, scale, loss, dlogits, ld_dlogits, ws, stream):
     f32, i32, dev = torch.float32, torch.int32, torch.cuda.current_device()
     _check(fn(n, k, t, _arg(logits, dev, (n - 1) * ld + k, dt), ld, _arg(labels, dev, n, i32), _arg(teacher_idx, dev, n * t, i32), _arg(teacher_val, dev, n * t, f32),
-              alpha, tau, scale, _arg(loss, dev, 3, f32), _arg(dlogits, dev, (n - 1) * ld_dlogits + k, dt), ld_dlogits, _ptr(ws), _bytes(ws),
+              alpha, tau, scale, _arg(loss, dev, 3, f32), _arg(dlogits, dev, (n - 1) * ld_dlogits + k, dt), ld_dlogits, _arg(ws, dev, 0), _bytes(ws),
               _stream(stream)))
 
 

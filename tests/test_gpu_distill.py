@@ -253,6 +253,15 @@ def test_distillation(n, k, t, alpha, tau, bf16):
 
 
 @pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("tau", [1 / 1024, 0.25, 16.0, 1024.0])
+@pytest.mark.parametrize("n,k,t", [(5, 9, 3), (6, 1000, 10), (4, 50021, 30)])
+def test_distillation_at_the_ends_of_the_temperatures(n, k, t, tau, bf16):
+    z = _rows(k, n, k, bf16)
+    idx, val = _teacher(k, z, t)
+    _check(z, np.arange(n), idx, val, 0.5, tau, 1 / n, bf16, pad=1)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("n,k,t", [(6, 50, 12), (6, 3001, 256), (6, 70001, 40), (300, 1030, 20)])
 def test_distillation_with_masked_classes_and_repeated_ones(n, k, t, bf16):
     """Classes masked by -infinity and by a very low value, a class kept several times, the label among the kept, logits far apart."""
