@@ -105,7 +105,7 @@ template <int ACT> __device__ inline float gn_act_bwd(float d, float u)
 }
 
 // ---- how threads lie over rows and channels ----------------------------------------------------------------------------------
-// A workgroup's rows have `cols` vectors.  Up to 64 of them: a wavefront has 64/cols rows side by side (lanes left over idle), and adds
+// A workgroup's rows have `cols` vectors.  Up to 32 of them: a wavefront has 64/cols rows side by side (lanes left over idle), and adds
 // them up with shuffles.  More: thread = row lane * cols + column.  Either way a thread stays in its column, and `slots` partial rows
 // per workgroup meet in LDS.
 struct GnMap {
@@ -114,8 +114,8 @@ struct GnMap {
     {
         GnMap m;
         m.cols = cols;
-        m.row_lanes = cols <= 64 ? 64 / cols * (threads / 64) : threads / cols;
-        m.slots = cols <= 64 ? threads / 64 : m.row_lanes;
+        m.row_lanes = cols <= 32 ? 64 / cols * (threads / 64) : threads / cols;
+        m.slots = cols <= 32 ? threads / 64 : m.row_lanes;
         return m;
     }
 };
@@ -124,7 +124,7 @@ struct GnThread {
     bool active;
     __device__ GnThread(const GnMap &m)
     {
-        if (m.cols <= 64) {
+        if (m.cols <= 32) {
             const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = 64 / m.cols;
             lane_row = lane / m.cols;
             col = lane - lane_row * m.cols;
@@ -187,22 +187,17 @@ __device__ inline float gn_total(float v, float *red)
         for (int u = 0; u < 4; ++u) s[u] += red[k + u];
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
-// Sums of runs of `run` of the W channels: groups[i] = sum of chan[i*run ..].  Few long runs: each the whole workgroup's work.  Ends with
-// a barrier.
-__device__ inline void gn_group_sums(int W, int run, const float *chan, float *groups, float *red)
+// Sums of runs of `run` of the W channels: groups[i] = sum of chan[i*run ..].  Long runs: a wavefront to each (the workgroup to one after
+// the other, with two barriers each: the forward pass of 25 x 22 x 22 x 1440 bf16 with groups of 45 took 55 us instead of 40).  Ends with a
+// barrier.
+__device__ inline void gn_group_sums(int W, int run, const float *chan, float *groups)
 {
     if (run > 32) {
-        for (int g = 0; g < W / run; ++g) {
+        for (int g = threadIdx.x >> 6; g < W / run; g += blockDim.x / 64) {
             float s = 0.f;
-            for (int c = threadIdx.x; c < run; c += blockDim.x) s += chan[g * run + c];
+            for (int c = threadIdx.x & 63; c < run; c += 64) s += chan[g * run + c];
             s = wave_sum(s);
-            __syncthreads();  // red has been read
-            if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                for (unsigned k = 1; k < blockDim.x / 64; ++k) s += red[k];
-                groups[g] = s;
-            }
+            if ((threadIdx.x & 63) == 0) groups[g] = s;
         }
     } else {
         for (int g = threadIdx.x; g < W / run; g += blockDim.x) {
@@ -226,7 +221,7 @@ struct GnShape {
 // sees channel c's and returns what stays of them.  Then their sums by group in grp: W/run of the one, W/run of the other.
 template <int V, class F>
 __device__ inline void gn_two_sums(const GnMap &m, const GnThread &t, const float (&a0)[V], const float (&a1)[V], int width, int run, float *part,
-                                   float *chan, float *grp, float *red, F f)
+                                   float *chan, float *grp, F f)
 {
     float both[2 * V];
 #pragma unroll
@@ -242,7 +237,7 @@ __device__ inline void gn_two_sums(const GnMap &m, const GnThread &t, const floa
         chan[width + c] = kept.y;
     }
     __syncthreads();
-    gn_group_sums(2 * width, run, chan, grp, red);
+    gn_group_sums(2 * width, run, chan, grp);
 }
 
 // S values of a vector that differ by group: one where vectors lie within groups (S == 1), else one to a channel.  Index of channel i's.
@@ -294,7 +289,7 @@ __global__ __launch_bounds__(TH) void gn_fwd_kernel(GnShape s, GnResident p, con
             return;
         }
         gn_column_sums<S>(p.map, t, v, part, chan);
-        gn_group_sums(p.W / PER, s.Cg / PER, chan, grp, red);
+        gn_group_sums(p.W / PER, s.Cg / PER, chan, grp);
 #pragma unroll
         for (int i = 0; i < S; ++i) v[i] = grp[(col + i) / s.Cg];
     };
@@ -426,7 +421,7 @@ __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, lon
 {
     typedef GnVec<T, V> Vec;
     extern __shared__ float lds[];
-    float *part = lds, *chan = part + 2 * p.map.slots * p.W, *red = chan + 2 * p.W, *grp = red + 32;
+    float *part = lds, *chan = part + 2 * p.map.slots * p.W, *grp = chan + 2 * p.W;
     const int id = xcd_contiguous(blockIdx.x, gridDim.x);
     const int n = s.n0 + id / p.chunks, c0 = id % p.chunks * p.W;
     const GnThread t(p.map);
@@ -457,7 +452,7 @@ __global__ __launch_bounds__(TH) void gn_bwd_kernel(GnShape s, GnResident p, lon
                 }
             }
     }
-    gn_two_sums<V>(p.map, t, a0, a1, p.W, s.Cg, part, chan, grp, red, [&](int i, float s0, float s1) {
+    gn_two_sums<V>(p.map, t, a0, a1, p.W, s.Cg, part, chan, grp, [&](int i, float s0, float s1) {
         sums[(long)n * s.C + c0 + i] = s0;
         sums[NC + (long)n * s.C + c0 + i] = s1;
         const float g = in.gamma[c0 + i];
@@ -543,7 +538,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnShape s, GnBands
     constexpr int PER = V / S;  // channels of a thread that share statistics
     extern __shared__ float lds[];
     const int sums = p.map.cols * S;  // a row's partial sums
-    float *part = lds, *chan = part + p.map.slots * sums, *red = chan + sums, *grp = red + 32;
+    float *part = lds, *chan = part + p.map.slots * sums, *grp = chan + sums;
     const GnPlace pl(s, p, blockIdx.x, gridDim.x);
     GnThread t(p.map);
     t.active = t.active && t.col * V < pl.width;
@@ -584,7 +579,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnShape s, GnBands
 #pragma unroll
     for (int i = 0; i < S; ++i) a[i] = mean[i] * (count * PER);
     gn_column_sums<S>(p.map, t, a, part, chan);
-    gn_group_sums(pl.width / PER, pl.run / PER, chan, grp, red);
+    gn_group_sums(pl.width / PER, pl.run / PER, chan, grp);
     const float m = (float)rows * (float)pl.run;
 #pragma unroll
     for (int i = 0; i < S; ++i) {
@@ -594,7 +589,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_stats_kernel(GnShape s, GnBands
     const int groups = pl.width / pl.run;
     for (int k = threadIdx.x; k < groups; k += kGnThreads) *pl.partial(s, p, parts, k) = grp[k] / m;
     gn_column_sums<S>(p.map, t, a, part, chan);  // its first barrier: every thread has read grp
-    gn_group_sums(pl.width / PER, pl.run / PER, chan, grp, red);
+    gn_group_sums(pl.width / PER, pl.run / PER, chan, grp);
     for (int k = threadIdx.x; k < groups; k += kGnThreads) *pl.partial(s, p, parts + p.plane, k) = grp[k];
 }
 
@@ -693,7 +688,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape s, GnBands 
                                                              float *__restrict__ parts)
 {
     extern __shared__ float lds[];
-    float *part = lds, *chan = part + 2 * p.map.slots * p.W, *red = chan + 2 * p.W, *grp = red + 32;
+    float *part = lds, *chan = part + 2 * p.map.slots * p.W, *grp = chan + 2 * p.W;
     const GnPlace pl(s, p, blockIdx.x, gridDim.x);
     GnThread t(p.map);
     t.active = t.active && t.col * V < pl.width;
@@ -723,7 +718,7 @@ __global__ __launch_bounds__(kGnThreads) void gn_sums_kernel(GnShape s, GnBands 
                 }
         }
     float *out = chans + ((long)n * p.bands + pl.band) * s.C + pl.c0;
-    gn_two_sums<V>(p.map, t, a0, a1, pl.width, pl.run, part, chan, grp, red, [&](int i, float s0, float s1) {
+    gn_two_sums<V>(p.map, t, a0, a1, pl.width, pl.run, part, chan, grp, [&](int i, float s0, float s1) {
         out[i] = s0;
         out[chan_plane + i] = s1;
         const float g = in.gamma[pl.c0 + i];
@@ -753,22 +748,31 @@ __global__ __launch_bounds__(kGnMergeThreads) void gn_sums_merge_kernel(GnShape 
     }
 }
 
-// dgamma and dbeta: sums over `rows` rows of C channels, a workgroup's 16 channels.  Thread = (row lane, channel); each adds every 32nd row,
-// four at a time; the row lanes are added in pairs, pairs of pairs, ...
-constexpr int kGnParamCh = 16, kGnParamRows = kGnThreads / kGnParamCh;
+// dgamma and dbeta: sums over `rows` rows of C channels, a workgroup's eight channels.  Thread = (row lane, channel); each adds every 32nd
+// row, eight at a time: bound by the latency of its loads, of a thousand rows four rounds of them (with 16 row lanes and four at a time, 16:
+// the backward pass of 63 x 14 x 27 x 280 bf16, whose workgroups behind these are done sooner, took 41 us instead of @@).  The row lanes are
+// added in pairs, pairs of pairs, ...
+constexpr int kGnParamCh = 8, kGnParamRows = kGnThreads / kGnParamCh, kGnParamBatch = 8;
 __device__ inline void gn_params(int block, long rows, int C, const float *__restrict__ chans, float *__restrict__ dgamma, float *__restrict__ dbeta,
                                  float (*red)[kGnThreads])
 {
     const int cl = threadIdx.x % kGnParamCh, rl = threadIdx.x / kGnParamCh, c = block * kGnParamCh + cl;
     float b[4] = {0.f, 0.f, 0.f, 0.f}, g[4] = {0.f, 0.f, 0.f, 0.f};
     if (c < C)
-        for (long r0 = rl; r0 < rows; r0 += 4 * kGnParamRows)
+        for (long r0 = rl; r0 < rows; r0 += kGnParamBatch * kGnParamRows) {
+            float v[kGnParamBatch], w[kGnParamBatch];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (r0 + u * kGnParamRows < rows) {
-                    b[u] += chans[(r0 + u * kGnParamRows) * C + c];
-                    g[u] += chans[(rows + r0 + u * kGnParamRows) * C + c];
-                }
+            for (int u = 0; u < kGnParamBatch; ++u) {
+                const long r = r0 + u * kGnParamRows;
+                v[u] = r < rows ? chans[r * C + c] : 0.f;
+                w[u] = r < rows ? chans[(rows + r) * C + c] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < kGnParamBatch; ++u) {
+                b[u % 4] += v[u];
+                g[u % 4] += w[u];
+            }
+        }
     red[0][threadIdx.x] = (b[0] + b[1]) + (b[2] + b[3]);
     red[1][threadIdx.x] = (g[0] + g[1]) + (g[2] + g[3]);
 #pragma unroll
