@@ -53,7 +53,8 @@ template <> struct GnVec<bf16_t, 8> {
 template <class T, int V> __device__ inline typename GnVec<T, V>::Raw gn_load(const T *p) { return *reinterpret_cast<const typename GnVec<T, V>::Raw *>(p); }
 template <class T, int V> __device__ inline void gn_store(T *p, const float *f) { *reinterpret_cast<typename GnVec<T, V>::Raw *>(p) = GnVec<T, V>::pack(f); }
 // The same past the caches' normal order of keeping lines.  For the second pass over memory: its results, and what it reads for the last
-// time, would push out what it has yet to read again.  32 x 112 x 112 x 64 fp32 backward 113 -> 95 us, 128 x 56 x 56 x 256 bf16 forward
+// time, would push out what it has yet to read again.  (Loads only where rows are whole cache lines, so that no line is wanted twice:
+// 13 x 97 x 97 x 156 bf16 backward with them 66 us, without 56.)  32 x 112 x 112 x 64 fp32 backward 113 -> 95 us, 128 x 56 x 56 x 256 bf16 forward
 // 150 -> 130 (stores alone 142), 3 x 129 x 131 x 320 forward 42 -> 36.  A workgroup that keeps its group reads nothing again: there
 // 64 x 14 x 14 x 1024 bf16 backward takes 45 us so instead of 43.
 template <class T, int V> struct GnWords {
@@ -491,6 +492,7 @@ struct GnBands {
     int pieces;       // pieces of a group
     int rows, bands;  // rows of a band (the last may be short), bands of an image
     long plane;       // floats of a plane of partial results
+    bool past;        // the second pass's loads go past the caches' order: rows are whole cache lines
 };
 struct GnPlace {
     int image, band, rows, c0, width;  // the workgroup's
@@ -659,12 +661,17 @@ __global__ __launch_bounds__(kGnThreads) void gn_apply_kernel(GnShape s, GnBands
     constexpr int B = kGnBatch;
     for (int r0 = t.row; r0 < rows; r0 += B * RL) {
         typename Vec::Raw xr[B], rr[B];
+        auto load = [&](auto past) {
+            auto get = [&](const T *q) { return decltype(past)::value ? gn_load_past<T, V>(q) : gn_load<T, V>(q); };
 #pragma unroll
-        for (int u = 0; u < B; ++u)
-            if (r0 + u * RL < rows) {
-                xr[u] = gn_load_past<T, V>(x + base + (long)(r0 + u * RL) * s.C);
-                if (RES) rr[u] = gn_load_past<T, V>(res + base + (long)(r0 + u * RL) * s.C);
-            }
+            for (int u = 0; u < B; ++u)
+                if (r0 + u * RL < rows) {
+                    xr[u] = get(x + base + (long)(r0 + u * RL) * s.C);
+                    if (RES) rr[u] = get(res + base + (long)(r0 + u * RL) * s.C);
+                }
+        };
+        if (p.past) load(std::true_type{});
+        else load(std::false_type{});
 #pragma unroll
         for (int u = 0; u < B; ++u)
             if (r0 + u * RL < rows) {
@@ -750,7 +757,7 @@ __global__ __launch_bounds__(kGnMergeThreads) void gn_sums_merge_kernel(GnShape 
 
 // dgamma and dbeta: sums over `rows` rows of C channels, a workgroup's eight channels.  Thread = (row lane, channel); each adds every 32nd
 // row, eight at a time: bound by the latency of its loads, of a thousand rows four rounds of them (with 16 row lanes and four at a time, 16:
-// the backward pass of 63 x 14 x 27 x 280 bf16, whose workgroups behind these are done sooner, took 41 us instead of @@).  The row lanes are
+// the backward pass of 63 x 14 x 27 x 280 bf16, whose workgroups behind these are done sooner, took 41 us instead of 30).  The row lanes are
 // added in pairs, pairs of pairs, ...
 constexpr int kGnParamCh = 8, kGnParamRows = kGnThreads / kGnParamCh, kGnParamBatch = 8;
 __device__ inline void gn_params(int block, long rows, int C, const float *__restrict__ chans, float *__restrict__ dgamma, float *__restrict__ dbeta,
@@ -820,9 +827,13 @@ __global__ __launch_bounds__(kGnThreads) void gn_bwd_apply_kernel(GnShape s, GnB
     constexpr int B = kGnBatch;
     for (int r0 = t.row; r0 < rows; r0 += B * RL) {
         GnDz<T, V, ACT, RES, DY2> q[B];
+        auto load = [&](auto past) {
 #pragma unroll
-        for (int u = 0; u < B; ++u)
-            if (r0 + u * RL < rows) q[u].template load<true>(in, base + (long)(r0 + u * RL) * s.C);
+            for (int u = 0; u < B; ++u)
+                if (r0 + u * RL < rows) q[u].template load<decltype(past)::value>(in, base + (long)(r0 + u * RL) * s.C);
+        };
+        if (p.past) load(std::true_type{});
+        else load(std::false_type{});
 #pragma unroll
         for (int u = 0; u < B; ++u)
             if (r0 + u * RL < rows) {
@@ -875,6 +886,7 @@ static GnBands gn_bands(int n, int HW, int C, int Cg, int V, long total)
     p.rows = ceil_div(HW, bands);
     p.bands = ceil_div(HW, p.rows);
     p.plane = (long)n * (C / Cg) * p.pieces * p.bands;
+    p.past = false;
     return p;
 }
 
@@ -1003,7 +1015,9 @@ static int gn_fwd_impl(const char *who, int n, int c, int h, int w, int layout, 
                 }))
                 return;
         }
-        const GnBands p = gn_bands(n, HW, c, Cg, V, gn_reduce_total(n)), pa = gn_bands(n, HW, c, Cg, V, gn_apply_total());
+        const GnBands p = gn_bands(n, HW, c, Cg, V, gn_reduce_total(n));
+        GnBands pa = gn_bands(n, HW, c, Cg, V, gn_apply_total());
+        pa.past = (long)c * sizeof(T) % 128 == 0;
         float *mean = save_mean ? save_mean : (float *)ws, *invstd = save_invstd ? save_invstd : mean + (size_t)n * groups;
         float *parts = (float *)ws + room.pairs;
         const size_t lds = gn_lds_floats(p.map, p.W, 1) * sizeof(float);
@@ -1074,7 +1088,9 @@ static int gn_bwd_impl(const char *who, int n, int c, int h, int w, int layout, 
                 }))
                 return;
         }
-        const GnBands p = gn_bands(n, HW, c, Cg, V, gn_reduce_total(n)), pa = gn_bands(n, HW, c, Cg, V, gn_apply_total());
+        const GnBands p = gn_bands(n, HW, c, Cg, V, gn_reduce_total(n));
+        GnBands pa = gn_bands(n, HW, c, Cg, V, gn_apply_total());
+        pa.past = (long)c * sizeof(T) % 128 == 0;
         const long rows = (long)n * p.bands;
         const size_t lds = gn_lds_floats(p.map, p.W, 2) * sizeof(float);
         const long finest = (long)pa.bands * pa.chunks;
