@@ -54,7 +54,7 @@ template <class T, int V> __device__ inline typename GnVec<T, V>::Raw gn_load(co
 template <class T, int V> __device__ inline void gn_store(T *p, const float *f) { *reinterpret_cast<typename GnVec<T, V>::Raw *>(p) = GnVec<T, V>::pack(f); }
 // The same past the caches' normal order of keeping lines.  For the second pass over memory: its results, and what it reads for the last
 // time, would push out what it has yet to read again.  (Loads only where rows are whole cache lines, so that no line is wanted twice:
-// 13 x 97 x 97 x 156 bf16 backward with them 66 us, without 56.)  32 x 112 x 112 x 64 fp32 backward 113 -> 95 us, 128 x 56 x 56 x 256 bf16 forward
+// 13 x 97 x 97 x 156 bf16 backward with them 66 us, without 56.)  32 x 112 x 112 x 64 fp32 backward 113 -> 95 us (now 85), 128 x 56 x 56 x 256 bf16 forward
 // 150 -> 130 (stores alone 142), 3 x 129 x 131 x 320 forward 42 -> 36.  A workgroup that keeps its group reads nothing again: there
 // 64 x 14 x 14 x 1024 bf16 backward takes 45 us so instead of 43.
 template <class T, int V> struct GnWords {
@@ -891,7 +891,7 @@ static GnBands gn_bands(int n, int HW, int C, int Cg, int V, long total)
 }
 
 // The passes that add up: as many workgroups as fit the chip at once (four to a compute unit), so that they end together; of more images
-// than that makes sense for, many rounds of them.  32 x 112 x 112 x 64 fp32 backward: 1024 workgroups 95 us, 2048 113.
+// than that makes sense for, many rounds of them.  32 x 112 x 112 x 64 fp32 backward as it was then: 1024 workgroups 95 us, 2048 113 (now 85).
 static long gn_reduce_total(int n) { return n <= 256 ? 1024 : 8192; }
 // The element-wise passes: small workgroups.
 static long gn_apply_total() { return 16384; }  // 1024 and 4096: 64 x 56 x 56 x 256 bf16 backward 146 and 148 us instead of 140
